@@ -207,6 +207,73 @@ rattn_status rattn_prefill_chunk(const rattn_params* p, int32_t pos0, const void
                                  const float* gamma_swa, const float* gamma_rla, void* k_ring, void* v_ring,
                                  float* state, void* o, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Packed rings: the window cache in 8 bits.
+ * A ring row of D features is D E4M3 numbers (the OCP 8-bit format with 4 exponent bits, no infinities, largest 448) and
+ * D/32 scale bytes; byte b of a block of 32 features is the factor 2^(b-127) (E8M0, b from 1 on).  The factor is the least
+ * one with which the largest finite feature of the block is at most 448, the numbers are the nearest ones (ties to even), so
+ * a stored feature is off by at most 2^-4 of itself, or by 2^-10 times the factor.  Infinities and NaN are stored as NaN.  What
+ * is stored is exact in bf16 and fp32, and packing what was unpacked gives the same values.
+ *   codes [N,Hkv,W,D], scales [N,Hkv,W,D/32], one byte each, 16-byte aligned.
+ *
+ * rattn_ring_pack / rattn_ring_unpack: both rings of N sequences, every slot, from and to the type p->dtype (p->Hq, the scale,
+ * eps and the feature map are not used but must be valid).  A program packs what rattn_prefill_export or the last
+ * rattn_prefill_chunk left, and unpacks to continue a prompt. */
+rattn_status rattn_ring_pack(const rattn_decode_params* p, const void* k_ring, const void* v_ring, void* k_codes,
+                             void* k_scale, void* v_codes, void* v_scale, void* stream);
+rattn_status rattn_ring_unpack(const rattn_decode_params* p, const void* k_codes, const void* k_scale, const void* v_codes,
+                               const void* v_scale, void* k_ring, void* v_ring, void* stream);
+
+/* rattn_decode_step over packed rings: the token leaving the window is folded into the state as its slot stands for it, the new
+ * one takes part in this step as given and is stored packed.  p->dtype is the type of q, k_new, v_new and o.  workspace as in
+ * rattn_decode_step_ws, of rattn_decode_packed_workspace_bytes() bytes, or NULL. */
+rattn_status rattn_decode_packed_workspace_bytes(const rattn_decode_params* p, size_t* bytes);
+rattn_status rattn_decode_step_packed(const rattn_decode_params* p, const void* q, const void* k_new, const void* v_new,
+                                      const int32_t* pos, void* k_codes, void* k_scale, void* v_codes, void* v_scale,
+                                      float* state, const float* gamma_swa, const float* gamma_rla, void* o,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Trees of drafted tokens (speculative decoding).  A slot that is overwritten and a key that is folded into the state
+ * cannot be taken back, so drafted tokens stay outside of the cache until they are accepted: rattn_tree_step computes the layer
+ * for all of them and only reads rings and state, rattn_tree_commit takes the accepted ones in. */
+typedef struct {
+  int32_t N;             /* sequences                                                          */
+  int32_t Hq, Hkv, D;
+  int32_t window;        /* W >= 1                                                             */
+  int32_t dtype;         /* of q, k, v, o (and of the rings, where they are not packed)        */
+  int32_t nodes;         /* M, 1 .. 64: drafted tokens per sequence that the tensors hold      */
+  float softmax_scale;
+  float rms_eps;
+  int32_t feature_map;
+} rattn_tree_params;
+
+/* The layer for node i < count[n] of every sequence n with pos[n] = p tokens in its cache: node i is the token at position
+ * p + (its depth), behind the cache's tokens and its own ancestors, and sees nothing of other branches.  With one node this is
+ * what rattn_decode_step returns for it.
+ *   q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M] (device): parent[n,i] < i is the node that i continues, -1 the
+ *     sequence's last token (any other value counts as -1)
+ *   count int32 [N] (device), NULL = M for all: nodes of each sequence; rows of o behind them are left as they are.  A sequence
+ *     with count[n] <= 0 or pos[n] < 0 has nothing done for it
+ *   pos int32 [N] (device); rings and state as rattn_decode_step finds them at pos: [N,Hkv,W,D] each and fp32 [N,Hkv,D,D].  The
+ *     state is read only if p > W (before that it is zero by definition)
+ *   k_scale, v_scale: NULL, or the scales of packed rings
+ *   o [N,M,Hq,D]
+ *   workspace: 16-byte aligned, rattn_tree_workspace_bytes() bytes (0 for steps that would not gain from it; `packed`: whether the
+ *     rings are), contents arbitrary, as in rattn_decode_step_ws; NULL: none is used. */
+rattn_status rattn_tree_workspace_bytes(const rattn_tree_params* p, int32_t packed, size_t* bytes);
+rattn_status rattn_tree_step(const rattn_tree_params* p, const void* q, const void* k, const void* v, const int32_t* parent,
+                             const int32_t* count, const int32_t* pos, const void* k_ring, const void* k_scale,
+                             const void* v_ring, const void* v_scale, const float* state, const float* gamma_swa,
+                             const float* gamma_rla, void* o, void* workspace, size_t workspace_bytes, void* stream);
+
+/* accepted[n] (int32 [N], device) is the last accepted node of sequence n; it and its ancestors, L of them, become tokens
+ * p .. p + L - 1: keys and values that leave the window are folded into the state (which is read only if p > W, and left as it is
+ * while nothing leaves), the others take their slots, packed where the rings are.  accepted[n] outside 0 .. M-1 or pos[n] < 0: the
+ * sequence's cache stays as it is.  pos is not written: the caller advances it by L when every layer is done.
+ * (softmax_scale and rms_eps are not used but must be valid.) */
+rattn_status rattn_tree_commit(const rattn_tree_params* p, const void* k, const void* v, const int32_t* parent,
+                               const int32_t* accepted, const int32_t* pos, void* k_ring, void* k_scale, void* v_ring,
+                               void* v_scale, float* state, void* stream);
+
 /* Closed forms of the paper's inference analysis (Sec. 4.4), evaluated on the HOST: nothing is launched, every
  * argument is a host value and the result is written to *out (HOST).
  *

@@ -360,6 +360,90 @@ def prefill_export(k, v, W, feature_map="softmax"):
     return k_ring, v_ring, state
 
 
+# ----------------------------------------------------------------------------- packed rings
+def pack_rows(x):
+    """(codes, scales) of rows [..., D]: per block of 32 features the least power of two, from 2^-126 on, with which the largest
+    finite |x| is at most 448, and the nearest E4M3 numbers (ties to even) of x over it, both as the values they stand for;
+    NaN where x is no finite number.  x = bf16 or fp32 values in float64."""
+    x = np.asarray(x, np.float64)
+    b = x.reshape(x.shape[:-1] + (-1, 32))
+    fin = np.isfinite(b)
+    a = np.max(np.abs(np.where(fin, b, 0.0)), axis=-1)
+    e = np.full(a.shape, -126)
+    while np.any(a > 448.0 * np.ldexp(1.0, e)):
+        e = e + (a > 448.0 * np.ldexp(1.0, e))
+    y = np.where(fin, b, 0.0) / np.ldexp(1.0, e)[..., None]
+    step = np.ldexp(1.0, np.maximum(np.frexp(y)[1] - 1, -6) - 3)     # spacing of the numbers around y
+    codes = np.where(fin, np.rint(y / step) * step, np.nan)
+    return codes.reshape(x.shape), np.ldexp(1.0, e)
+
+
+def packed_values(codes, scales):
+    return np.asarray(codes, np.float64) * np.repeat(np.asarray(scales, np.float64), 32, axis=-1)
+
+
+# ----------------------------------------------------------------------------- trees of drafted tokens
+def tree_path(parent, i):
+    """Node i and its ancestors, the first token first."""
+    path = []
+    while i >= 0:
+        path.append(i)
+        i = int(parent[i]) if 0 <= parent[i] < i else -1
+    return path[::-1]
+
+
+def tree_step(q, k, v, parent, pos, k_ring, v_ring, state, W, scale=1.0, eps=1e-6, gamma_swa=None, gamma_rla=None,
+              feature_map="softmax", count=None):
+    """The layer (Sec. 2.1, Eq. 4, Sec. 3.2) at every node of a tree of drafted tokens: node i is the last token of the sequence
+    [the pos[n] tokens of the cache ; path to i].  Rings hold the last min(pos, W) tokens, `state` the sum over the tokens
+    before pos - W.  q [N,M,Hq,D], k, v [N,M,Hkv,D], parent [N,M]; rows of nodes from count[n] on are NaN."""
+    q = np.asarray(q, np.float64); k = np.asarray(k, np.float64); v = np.asarray(v, np.float64)
+    N, M, Hq, D = q.shape
+    Hkv = k.shape[2]; G = Hq // Hkv
+    gs = _gains(gamma_swa, Hq, D); gr = _gains(gamma_rla, Hq, D)
+    o = np.full((N, M, Hq, D), np.nan)
+    for n in range(N):
+        p = int(pos[n])
+        old = [s % W for s in range(max(0, p - W), p)]
+        for i in range(M if count is None else int(count[n])):
+            path = tree_path(parent[n], i)
+            for g in range(Hkv):
+                keys = np.concatenate([k_ring[n, g, old], k[n, path, g]])
+                vals = np.concatenate([v_ring[n, g, old], v[n, path, g]])
+                cut = max(0, len(keys) - W)        # tokens that have left this node's window
+                for h in range(g * G, (g + 1) * G):
+                    a = scale * (keys[cut:] @ q[n, i, h])
+                    e = np.exp(a - a.max())
+                    x_s = (e / e.sum()) @ vals[cut:]
+                    f = phi(q[n, i, h], feature_map)
+                    x_r = (phi(keys[:cut], feature_map) @ f) @ vals[:cut] if cut else np.zeros(D)
+                    if p > W:
+                        x_r = x_r + f @ state[n, g]
+                    o[n, i, h] = rms(x_s, gs[h], eps)[0] + rms(x_r, gr[h], eps)[0]
+    return o
+
+
+def tree_commit(k, v, parent, accepted, pos, k_ring, v_ring, state, W, feature_map="softmax"):
+    """The cache after the tokens of the path to node accepted[n] (-1: none): rings, and the state over every token that is W or more
+    back by then.  Returns new arrays; a slot's content is the token's key or value as given."""
+    k_ring = np.array(k_ring, np.float64); v_ring = np.array(v_ring, np.float64); state = np.array(state, np.float64)
+    k = np.asarray(k, np.float64); v = np.asarray(v, np.float64)
+    M, Hkv = k.shape[1:3]
+    for n in range(k.shape[0]):
+        p = int(pos[n])
+        if p < 0 or not 0 <= accepted[n] < M:
+            continue
+        for d, i in enumerate(tree_path(parent[n], int(accepted[n]))):
+            slot = (p + d) % W
+            for g in range(Hkv):
+                if p + d >= W:
+                    if p + d == W:
+                        state[n, g] = 0.0
+                    state[n, g] += np.outer(phi(k_ring[n, g, slot], feature_map), v_ring[n, g, slot])
+                k_ring[n, g, slot] = k[n, i, g]; v_ring[n, g, slot] = v[n, i, g]
+    return k_ring, v_ring, state
+
+
 # ----------------------------------------------------------------------------- closed forms in the text
 def kv_cache_saving(layers, global_every, ctx, w_from, w_to):
     """Fraction of KV cache saved when local layers shrink their window (Sec. 1 example):

@@ -28,6 +28,8 @@ EXPORTS = ["rattn_workspace_bytes", "rattn_fwd", "rattn_fwd_static", "rattn_bwd"
            "rattn_decode_workspace_bytes", "rattn_decode_step_ws",
            "rattn_prefill_export_workspace_bytes", "rattn_prefill_export",
            "rattn_prefill_chunk_workspace_bytes", "rattn_prefill_chunk", "rattn_probe_mfma",
+           "rattn_ring_pack", "rattn_ring_unpack", "rattn_decode_packed_workspace_bytes", "rattn_decode_step_packed",
+           "rattn_tree_workspace_bytes", "rattn_tree_step", "rattn_tree_commit",
            "rattn_cache_bytes", "rattn_step_time_model",
            "rattn_status_string", "rattn_last_error", "rattn_version",
            "rattn_profile_enable", "rattn_profile_reset", "rattn_profile_count", "rattn_profile_get"]
@@ -45,6 +47,12 @@ class RattnDecodeParams(ctypes.Structure):
     _fields_ = [("N", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("window", ctypes.c_int32), ("dtype", ctypes.c_int32), ("softmax_scale", ctypes.c_float),
                 ("rms_eps", ctypes.c_float), ("feature_map", ctypes.c_int32)]
+
+
+class RattnTreeParams(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("dtype", ctypes.c_int32), ("nodes", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("rms_eps", ctypes.c_float), ("feature_map", ctypes.c_int32)]
 
 
 class RattnError(RuntimeError):
@@ -88,6 +96,18 @@ def lib():
     L.rattn_prefill_chunk_workspace_bytes.argtypes = [ctypes.POINTER(RattnParams), ctypes.c_int32, ctypes.POINTER(sz)]
     L.rattn_prefill_chunk.restype = ctypes.c_int
     L.rattn_prefill_chunk.argtypes = [ctypes.POINTER(RattnParams), ctypes.c_int32] + [vp] * 10 + [sz, vp]
+    L.rattn_ring_pack.restype = L.rattn_ring_unpack.restype = ctypes.c_int
+    L.rattn_ring_pack.argtypes = L.rattn_ring_unpack.argtypes = [ctypes.POINTER(RattnDecodeParams)] + [vp] * 7
+    L.rattn_decode_packed_workspace_bytes.restype = ctypes.c_int
+    L.rattn_decode_packed_workspace_bytes.argtypes = [ctypes.POINTER(RattnDecodeParams), ctypes.POINTER(sz)]
+    L.rattn_decode_step_packed.restype = ctypes.c_int
+    L.rattn_decode_step_packed.argtypes = [ctypes.POINTER(RattnDecodeParams)] + [vp] * 13 + [sz, vp]
+    L.rattn_tree_workspace_bytes.restype = ctypes.c_int
+    L.rattn_tree_workspace_bytes.argtypes = [ctypes.POINTER(RattnTreeParams), ctypes.c_int32, ctypes.POINTER(sz)]
+    L.rattn_tree_step.restype = ctypes.c_int
+    L.rattn_tree_step.argtypes = [ctypes.POINTER(RattnTreeParams)] + [vp] * 15 + [sz, vp]
+    L.rattn_tree_commit.restype = ctypes.c_int
+    L.rattn_tree_commit.argtypes = [ctypes.POINTER(RattnTreeParams)] + [vp] * 11
     L.rattn_cache_bytes.restype = ctypes.c_int
     L.rattn_cache_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
                                     ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_double)]
@@ -382,6 +402,174 @@ def rattn_prefill_chunk(q, k, v, window, pos0, k_ring, v_ring, state, gamma_swa=
     _check(lib().rattn_prefill_chunk(p, pos0, _ptr(q), _ptr(k), _ptr(v), _ptr(gs), _ptr(gr), _ptr(k_ring), _ptr(v_ring),
                                      _ptr(state), _ptr(o), _ptr(workspace), workspace.numel(), _stream()))
     return o
+
+
+# ---- packed rings and trees of drafted tokens
+PACKED_DTYPES = (torch.float8_e4m3fn, torch.float8_e8m0fnu)   # codes [N,Hkv,W,D], scales [N,Hkv,W,D/32]
+
+
+def _on_device(dev, **tensors):
+    """Contiguous device tensors, all on the current device `dev`."""
+    for name, t in tensors.items():
+        if t is not None and not (t.is_cuda and t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous device tensor")
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} must be on the device of the other tensors")
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, which is not the current device")
+
+
+def _check_packed(N, Hkv, W, D, k_codes, k_scale, v_codes, v_scale):
+    for name, t, dt, n in (("k_codes", k_codes, 0, D), ("k_scale", k_scale, 1, D // 32), ("v_codes", v_codes, 0, D),
+                           ("v_scale", v_scale, 1, D // 32)):
+        if t.shape != (N, Hkv, W, n) or t.dtype != PACKED_DTYPES[dt]:
+            raise ValueError(f"{name} must be {PACKED_DTYPES[dt]} {[N, Hkv, W, n]}")
+
+
+@functools.lru_cache(maxsize=64)
+def _ring_plan(shape, dtype):
+    N, Hkv, W, D = shape
+    return ctypes.byref(RattnDecodeParams(N, Hkv, Hkv, D, W, _DTYPES[dtype], 1.0, 1e-6, 0))
+
+
+def rattn_ring_pack(k_ring, v_ring, out=None):
+    """Rings [N,Hkv,W,D] in 8 bits: (k_codes, k_scale, v_codes, v_scale), codes float8_e4m3fn [N,Hkv,W,D] and scales
+    float8_e8m0fnu [N,Hkv,W,D/32]; a feature is its code times the scale of its 32 features.  `out`: those four, to be reused."""
+    if k_ring.dim() != 4 or v_ring.shape != k_ring.shape or k_ring.dtype not in _DTYPES or v_ring.dtype != k_ring.dtype:
+        raise ValueError("k_ring and v_ring must share shape [N,Hkv,W,D] and dtype float32 or bfloat16")
+    N, Hkv, W, D = k_ring.shape
+    if out is None:
+        out = tuple(torch.empty(N, Hkv, W, n, dtype=dt, device=k_ring.device)
+                    for n, dt in ((D, PACKED_DTYPES[0]), (D // 32, PACKED_DTYPES[1])) * 2)
+    kc, ks, vc, vs = out
+    _on_device(k_ring.device, k_ring=k_ring, v_ring=v_ring, k_codes=kc, k_scale=ks, v_codes=vc, v_scale=vs)
+    _check_packed(N, Hkv, W, D, kc, ks, vc, vs)
+    _check(lib().rattn_ring_pack(_ring_plan(k_ring.shape, k_ring.dtype), _ptr(k_ring), _ptr(v_ring), _ptr(kc), _ptr(ks), _ptr(vc),
+                                 _ptr(vs), _stream()))
+    return out
+
+
+def rattn_ring_unpack(k_codes, k_scale, v_codes, v_scale, dtype=torch.bfloat16, out=None):
+    """(k_ring, v_ring) in `dtype` of packed rings; both types hold what is packed exactly.  `out`: the two, to be reused."""
+    if k_codes.dim() != 4 or dtype not in _DTYPES:
+        raise ValueError("codes must be [N,Hkv,W,D] and dtype float32 or bfloat16")
+    shape = k_codes.shape
+    _check_packed(*shape, k_codes, k_scale, v_codes, v_scale)
+    kr, vr = (torch.empty(shape, dtype=dtype, device=k_codes.device) for _ in range(2)) if out is None else out
+    if kr.shape != shape or vr.shape != shape or kr.dtype != dtype or vr.dtype != dtype:
+        raise ValueError("out must be two rings of the codes' shape in `dtype`")
+    _on_device(k_codes.device, k_codes=k_codes, k_scale=k_scale, v_codes=v_codes, v_scale=v_scale, k_ring=kr, v_ring=vr)
+    _check(lib().rattn_ring_unpack(_ring_plan(shape, dtype), _ptr(k_codes), _ptr(k_scale), _ptr(v_codes), _ptr(v_scale), _ptr(kr),
+                                   _ptr(vr), _stream()))
+    return kr, vr
+
+
+@functools.lru_cache(maxsize=64)
+def _packed_plan(q_shape, Hkv, window, dtype, softmax_scale, rms_eps, feature_map):
+    N, Hq, D = q_shape
+    p = RattnDecodeParams(N, Hq, Hkv, D, window, _DTYPES[dtype], softmax_scale, rms_eps, FEATURE_MAPS[feature_map])
+    nbytes = ctypes.c_size_t()
+    _check(lib().rattn_decode_packed_workspace_bytes(ctypes.byref(p), ctypes.byref(nbytes)))
+    return ctypes.byref(p), nbytes.value
+
+
+def _check_out(out, q):
+    if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor like q")
+    return out
+
+
+def rattn_decode_step_packed(q, k_new, v_new, pos, k_codes, k_scale, v_codes, v_scale, state, gamma_swa=None, gamma_rla=None,
+                             softmax_scale=1.0, rms_eps=1e-6, out=None, feature_map="softmax"):
+    """rattn_decode_step over packed rings (see rattn_ring_pack), which are updated in place as the state is; returns o [N,Hq,D]."""
+    N, Hq, D = q.shape
+    Hkv, W = k_codes.shape[1:3]
+    _on_device(q.device, q=q, k_new=k_new, v_new=v_new, pos=pos, k_codes=k_codes, k_scale=k_scale, v_codes=v_codes, v_scale=v_scale,
+               state=state)
+    if k_new.shape != (N, Hkv, D) or v_new.shape != k_new.shape or state.shape != (N, Hkv, D, D) or pos.shape != (N,):
+        raise ValueError("decode tensor shapes do not match")
+    _check_packed(N, Hkv, W, D, k_codes, k_scale, v_codes, v_scale)
+    if state.dtype != torch.float32 or pos.dtype != torch.int32:
+        raise ValueError("state must be float32 and pos int32")
+    if q.dtype not in _DTYPES or k_new.dtype != q.dtype or v_new.dtype != q.dtype:
+        raise ValueError("q, k_new and v_new must share dtype float32 or bfloat16")
+    p, nbytes = _packed_plan(q.shape, Hkv, W, q.dtype, float(softmax_scale), float(rms_eps), feature_map)
+    gs, gr = _gain(gamma_swa, Hq, D, q.device), _gain(gamma_rla, Hq, D, q.device)
+    o = torch.empty_like(q) if out is None else _check_out(out, q)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+    _check(lib().rattn_decode_step_packed(p, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(pos), _ptr(k_codes), _ptr(k_scale),
+                                          _ptr(v_codes), _ptr(v_scale), _ptr(state), _ptr(gs), _ptr(gr), _ptr(o), _ptr(ws), nbytes,
+                                          _stream()))
+    return o
+
+
+TREE_MAX_NODES = 64
+
+
+@functools.lru_cache(maxsize=64)
+def _tree_plan(k_shape, Hq, window, dtype, packed, softmax_scale, rms_eps, feature_map):
+    N, M, Hkv, D = k_shape
+    p = RattnTreeParams(N, Hq, Hkv, D, window, _DTYPES[dtype], M, softmax_scale, rms_eps, FEATURE_MAPS[feature_map])
+    nbytes = ctypes.c_size_t()
+    _check(lib().rattn_tree_workspace_bytes(ctypes.byref(p), 1 if packed else 0, ctypes.byref(nbytes)))
+    return ctypes.byref(p), nbytes.value
+
+
+def _check_tree(k, v, parent, pos, k_ring, v_ring, state, k_scale, v_scale, **more):
+    if k.dim() != 4 or v.shape != k.shape or k.dtype not in _DTYPES or v.dtype != k.dtype:
+        raise ValueError("k and v must share shape [N,M,Hkv,D] and dtype float32 or bfloat16")
+    N, M, Hkv, D = k.shape
+    _on_device(k.device, k=k, v=v, parent=parent, pos=pos, k_ring=k_ring, v_ring=v_ring, state=state, k_scale=k_scale,
+               v_scale=v_scale, **more)
+    if k_ring.dim() != 4 or state.shape != (N, Hkv, D, D) or state.dtype != torch.float32:
+        raise ValueError("rings must be [N,Hkv,W,D] and state float32 [N,Hkv,D,D]")
+    W = k_ring.shape[2]
+    if (k_scale is None) != (v_scale is None):
+        raise ValueError("packed rings have k_scale and v_scale, others neither")
+    if k_scale is not None:
+        _check_packed(N, Hkv, W, D, k_ring, k_scale, v_ring, v_scale)
+    elif k_ring.shape != (N, Hkv, W, D) or v_ring.shape != k_ring.shape or k_ring.dtype != k.dtype or v_ring.dtype != k.dtype:
+        raise ValueError("k_ring and v_ring must be [N,Hkv,W,D] in the dtype of k and v (or packed, with their scales)")
+    if parent.shape != (N, M) or parent.dtype != torch.int32 or pos.shape != (N,) or pos.dtype != torch.int32:
+        raise ValueError("parent must be int32 [N,M] and pos int32 [N]")
+    for name, t in more.items():
+        if name in ("count", "accepted") and t is not None and (t.shape != (N,) or t.dtype != torch.int32):
+            raise ValueError(f"{name} must be int32 [N]")
+    return W
+
+
+def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None, gamma_rla=None, softmax_scale=1.0,
+                    rms_eps=1e-6, count=None, k_scale=None, v_scale=None, out=None, feature_map="softmax"):
+    """The layer for a tree of up to 64 drafted tokens behind each of N sequences; rings and state are only read.
+
+    q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M]: the earlier node that a node continues, -1 = the sequence's last token;
+    pos int32 [N]: tokens in the cache; count int32 [N]: nodes of each sequence (None: M), rows behind them are left as they are
+    in `out` (zero where it is allocated here).  k_scale, v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
+    if q.dim() != 4 or q.dtype != k.dtype or k.dim() != 4 or (q.shape[0], q.shape[1], q.shape[3]) != (k.shape[0], k.shape[1], k.shape[3]):
+        raise ValueError("q must be [N,M,Hq,D] like k and v [N,M,Hkv,D], in their dtype")
+    W = _check_tree(k, v, parent, pos, k_ring, v_ring, state, k_scale, v_scale, q=q, count=count)
+    Hq, D = q.shape[2:]
+    p, nbytes = _tree_plan(k.shape, Hq, W, k.dtype, k_scale is not None, float(softmax_scale), float(rms_eps), feature_map)
+    gs, gr = _gain(gamma_swa, Hq, D, q.device), _gain(gamma_rla, Hq, D, q.device)
+    if out is None:
+        o = torch.empty_like(q) if count is None else torch.zeros_like(q)
+    else:
+        o = _check_out(out, q)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None
+    _check(lib().rattn_tree_step(p, _ptr(q), _ptr(k), _ptr(v), _ptr(parent), _ptr(count), _ptr(pos), _ptr(k_ring), _ptr(k_scale),
+                                 _ptr(v_ring), _ptr(v_scale), _ptr(state), _ptr(gs), _ptr(gr), _ptr(o), _ptr(ws), nbytes, _stream()))
+    return o
+
+
+def rattn_tree_commit(k, v, parent, accepted, pos, k_ring, v_ring, state, k_scale=None, v_scale=None, feature_map="softmax"):
+    """The accepted node of each sequence's tree and its ancestors become tokens of the cache: rings (packed where scales are
+    given) and state are updated in place.  accepted int32 [N]: node, or -1 for none.  pos is left to the caller, who advances it by
+    the length of the accepted path when every layer is done."""
+    W = _check_tree(k, v, parent, pos, k_ring, v_ring, state, k_scale, v_scale, accepted=accepted)
+    p, _ = _tree_plan(k.shape, k.shape[2], W, k.dtype, k_scale is not None, 1.0, 1e-6, feature_map)
+    _check(lib().rattn_tree_commit(p, _ptr(k), _ptr(v), _ptr(parent), _ptr(accepted), _ptr(pos), _ptr(k_ring), _ptr(k_scale),
+                                   _ptr(v_ring), _ptr(v_scale), _ptr(state), _stream()))
 
 
 def rattn_cache_bytes(layers, global_every, ctx, window, with_state, Hkv, D, elem_bytes):

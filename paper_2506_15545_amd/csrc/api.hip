@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include "host_api.hpp"
 #include "kernels.hpp"
 #include "rattn.h"
 
@@ -34,9 +35,10 @@ void prof_end(hipStream_t st) {
 }  // namespace rattn
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
 
+namespace rattn {
 rattn_status fail(rattn_status s, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
@@ -44,9 +46,20 @@ rattn_status fail(rattn_status s, const char* fmt, ...) {
   va_end(ap);
   return s;
 }
+rattn_status check_launch(const char* what) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(RATTN_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  return RATTN_OK;
+}
+}  // namespace rattn
+
+using rattn::fail;
+using rattn::check_launch;
+using rattn::aligned16;
+
+namespace {
 
 inline size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Sequence lengths from this size on run on the matrix-core kernels (bf16) whether or not they are a multiple of
 // the 128-row tile.  Shorter ones (less than one tile) stay on the general kernels.
@@ -255,12 +268,6 @@ rattn_status make_chunk_layout(const rattn_params* p, int32_t pos0, ChunkLayout*
   return RATTN_OK;
 }
 
-rattn_status check_launch(const char* what) {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(RATTN_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-  return RATTN_OK;
-}
-
 }  // namespace
 
 extern "C" {
@@ -429,7 +436,8 @@ rattn_status rattn_bwd(const rattn_params* p, const void* q, const void* k, cons
   return check_launch("rattn_bwd");
 }
 
-namespace {
+}  // extern "C"
+namespace rattn {
 rattn_status decode_dims(const rattn_decode_params* p, rattn::DecodeDims* dd) {
   if (!p) return fail(RATTN_ERR_INVALID_ARG, "params is NULL");
   if (p->N < 1 || p->Hq < 1 || p->Hkv < 1)
@@ -457,7 +465,10 @@ unsigned long long decode_nonce() {
   static unsigned long long count = 0;
   return (__atomic_add_fetch(&count, 1, __ATOMIC_RELAXED) * 0x9E3779B97F4A7C15ull) << 8;
 }
-}  // namespace
+}  // namespace rattn
+extern "C" {
+using rattn::decode_dims;
+using rattn::decode_nonce;
 
 rattn_status rattn_decode_workspace_bytes(const rattn_decode_params* p, size_t* bytes) {
   rattn::DecodeDims dd;

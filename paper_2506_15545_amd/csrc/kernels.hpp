@@ -223,4 +223,40 @@ void decode_step(const DecodeDims& dd, int dtype, const void* q, const void* k_n
                  const int32_t* pos, void* k_ring, void* v_ring, float* state, const float* gs, const float* gr,
                  void* o, hipStream_t st);
 
+// rings between the type of the tensors and 8 bits (packed.hpp); elements: of one of the two rings, a multiple of 64
+void ring_pack(int dtype, long long elements, const void* k, const void* v, void* kc, void* ks, void* vc, void* vs, hipStream_t st);
+void ring_unpack(int dtype, long long elements, const void* kc, const void* ks, const void* vc, const void* vs, void* k, void* v,
+                 hipStream_t st);
+// decode_step over packed rings; dd as for decode_step, dtype of the other tensors (decode_split: 1 byte an element)
+void decode_step_packed(const DecodeDims& dd, int dtype, const void* q, const void* k_new, const void* v_new, const int32_t* pos,
+                        void* k_ring, void* k_scale, void* v_ring, void* v_scale, float* state, const float* gs, const float* gr,
+                        void* o, hipStream_t st);
+
+// trees of drafted tokens (tree_kernels.hip, tree_commit.hip)
+struct TreeDims {
+  int N, M, Hq, Hkv, D, W, G;
+  float scale, eps;
+  int phi;
+  void* workspace = nullptr;       // NULL, or tree_plan(..).bytes
+  unsigned long long nonce = 0;    // as in DecodeDims
+};
+struct TreeTensors {
+  const void *q, *k, *v;
+  const int32_t *parent, *count, *pos;   // count may be NULL
+  void *k_ring, *k_scale, *v_ring, *v_scale;   // scales NULL: rings in the type of the tensors
+  void* state;
+  const float *gs, *gr;
+  void* o;
+};
+// How a tree step is cut: a work-group of NW waves has (NW / KG) groups of 16 CT rows (a row is a query head of a node; the rows of a
+// (sequence, KV head) are its nodes' heads in order), each shared by KG waves that divide the keys; `blocks` work-groups for all
+// rows of a pair, and `nsplit` for the keys of each.
+struct TreePlan {
+  int CT, KG, NW, blocks, nsplit;
+  size_t part_off, bytes;   // workspace: tickets from offset 0 (nothing: 0 bytes)
+};
+TreePlan tree_plan(const TreeDims& td, int dtype, bool packed);
+void tree_step(const TreeDims& td, int dtype, const TreeTensors& t, hipStream_t st);
+void tree_commit(const TreeDims& td, int dtype, const TreeTensors& t, const int32_t* accepted, hipStream_t st);
+
 }  // namespace rattn

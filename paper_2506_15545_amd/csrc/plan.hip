@@ -146,4 +146,26 @@ ExportPlan export_plan(const LayerDims& dm) {
   return pl;
 }
 
+TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
+  TreePlan p = {1, 8, 8, 1, 1, 0, 0};
+  const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32;
+  if (dtype == 0) {
+    p.KG = rows <= 16 ? 8 : rows <= 32 ? 4 : 2;
+  } else if (rows > 16) {
+    p.CT = 2;
+    p.KG = rows <= 32 ? 8 : rows <= 64 ? 4 : 2;
+  }
+  const int per = p.NW / p.KG * 16 * p.CT;
+  p.blocks = (rows + per - 1) / per;
+  const long long groups = (long long)td.N * td.Hkv * p.blocks;
+  const int sets = (td.W + keys - 1) / keys + (td.M + keys - 1) / keys;
+  p.nsplit = DEC_MAX_SPLIT;
+  while (p.nsplit > 1 && (groups * p.nsplit > 256 || sets < p.KG * p.nsplit)) p.nsplit /= 2;
+  if (p.nsplit > 1) {
+    p.part_off = ((size_t)groups * 8 + 255) / 256 * 256;
+    p.bytes = p.part_off + (size_t)groups * p.nsplit * per * (2 * td.D + 4) * 4;
+  }
+  return p;
+}
+
 }  // namespace rattn
