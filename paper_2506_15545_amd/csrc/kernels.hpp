@@ -249,10 +249,10 @@ struct TreeTensors {
   void* o;
 };
 // How a tree step is cut: a work-group of NW waves has (NW / KG) groups of 16 CT rows (a row is a query head of a node; the rows of a
-// (sequence, KV head) are its nodes' heads in order), each shared by KG waves that divide the keys; `blocks` work-groups for all
-// rows of a pair, and `nsplit` for the keys of each.
+// (sequence, KV head) are its nodes' heads in order), each shared by KG waves that divide the keys, KW of them those of the softmax
+// branch; `blocks` work-groups for all rows of a pair, and `nsplit` for the keys of each.
 struct TreePlan {
-  int CT, KG, NW, blocks, nsplit;
+  int CT, KG, NW, blocks, nsplit, KW;
   size_t part_off, bytes;   // workspace: tickets from offset 0 (nothing: 0 bytes)
 };
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed);

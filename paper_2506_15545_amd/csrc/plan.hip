@@ -147,20 +147,28 @@ ExportPlan export_plan(const LayerDims& dm) {
 }
 
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
-  TreePlan p = {1, 8, 8, 1, 1, 0, 0};
+  TreePlan p = {1, 8, 8, 1, 1, 6, 0, 0};
   const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32;
   if (dtype == 0) {
-    p.KG = rows <= 16 ? 8 : rows <= 32 ? 4 : 2;
+    p.KG = rows <= 16 ? 8 : 4;
   } else if (rows > 16) {
     p.CT = 2;
-    p.KG = rows <= 32 ? 8 : rows <= 64 ? 4 : 2;
+    p.KG = rows <= 32 ? 8 : 4;
   }
-  const int per = p.NW / p.KG * 16 * p.CT;
+  const int group = 16 * p.CT;
+  const long long pairs = (long long)td.N * td.Hkv;
+  if (rows <= group && pairs >= 256) p.KG = p.NW = 4;
+  const int per = p.NW / p.KG * group;
   p.blocks = (rows + per - 1) / per;
-  const long long groups = (long long)td.N * td.Hkv * p.blocks;
-  const int sets = (td.W + keys - 1) / keys + (td.M + keys - 1) / keys;
+  const long long groups = pairs * p.blocks;
+  const int sets = (td.W + keys - 1) / keys + (td.M + keys - 1) / keys, pieces = td.D / keys + 1;
+  // waves by what either branch has to do: a piece of the state counts one and a half sets of keys
+  int kl = (int)((p.KG * 3ll * pieces + (2 * sets + 3 * pieces) / 2) / (2 * sets + 3 * pieces));
+  if (kl < 1) kl = 1;
+  if (kl > p.KG / 2) kl = p.KG / 2;
+  p.KW = p.KG - kl;
   p.nsplit = DEC_MAX_SPLIT;
-  while (p.nsplit > 1 && (groups * p.nsplit > 256 || sets < p.KG * p.nsplit)) p.nsplit /= 2;
+  while (p.nsplit > 1 && (groups * p.nsplit > 256 || sets < p.KW * p.nsplit)) p.nsplit /= 2;
   if (p.nsplit > 1) {
     p.part_off = ((size_t)groups * 8 + 255) / 256 * 256;
     p.bytes = p.part_off + (size_t)groups * p.nsplit * per * (2 * td.D + 4) * 4;

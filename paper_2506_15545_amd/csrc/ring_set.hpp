@@ -308,6 +308,13 @@ struct NoSplit {
 // work-group: 12.0 -> 22.8 us at 16 work-groups for each of 4 pairs, 24 -> 83 at 4 for 256, where this way takes 18.2 and 30.4.
 __device__ __forceinline__ void put_shared(float* p, float x) { __hip_atomic_store(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float get_shared(const float* p) { return __hip_atomic_load(const_cast<float*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// 16 bytes in one access (bit 4: agent scope)
+__device__ __forceinline__ void put_shared16(rsrc_t r, f32x4_t v, int off) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), r, off, 0, 16);
+}
+__device__ __forceinline__ f32x4_t get_shared16(rsrc_t r, int off) {
+  return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 16));
+}
 // Called by the whole work-group after its put_shared; true in the one that arrives last, whose get_shared then see everyone's
 __device__ __forceinline__ bool arrive_last(unsigned long long* ticket, unsigned long long nonce, int n) {
   __shared__ int last;

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(NT) void tree_commit_kernel(const IO* __restrict__ 
   const int g = blockIdx.x, n = blockIdx.y, lane = lane_id(), w = wave_id();
   const int acc = accepted[n], p = pos[n];
   if (acc < 0 || acc >= M || p < 0) return;
-  const TreeNodes t = tree_nodes(parent + (size_t)n * M, M, W, lane);
+  const TreeNodes t = tree_nodes(lane < M ? parent[(size_t)n * M + lane] : -1, W, lane);
   const unsigned long long path = shfl64(t.anc, acc);   // parents come first: bits in the order of depth
   const int L = __popcll(path);
   const int first = max(0, W - p), E = L - first;   // leaving: j = first .. L - 1, token p - W + j

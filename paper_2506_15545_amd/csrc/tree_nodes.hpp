@@ -16,11 +16,10 @@ struct TreeNodes {
   unsigned long long left;   // those of them that are W or more tokens back
   __device__ __forceinline__ int depth() const { return __popcll(anc) - 1; }
 };
-// parent: of this sequence, m of them.  A parent that is no earlier node counts as the sequence's last token (-1).  Called by
-// whole waves.  Six rounds that double the distance: `jump` is the ancestor 2^r back, `far` the one W back.
-__device__ __forceinline__ TreeNodes tree_nodes(const int32_t* parent, int m, int W, int lane) {
-  int jump = lane < m ? parent[lane] : -1;
-  if (jump < 0 || jump >= lane) jump = -1;
+// parent: of node `lane` (anything for lanes without one).  A parent that is no earlier node counts as the sequence's last token
+// (-1).  Called by whole waves.  Six rounds that double the distance: `jump` is the ancestor 2^r back, `far` the one W back.
+__device__ __forceinline__ TreeNodes tree_nodes(int parent, int W, int lane) {
+  int jump = parent < 0 || parent >= lane ? -1 : parent;
   int far = W < TREE_MAX_NODES ? lane : -1;
   TreeNodes t;
   t.anc = 1ull << lane;
