@@ -36,7 +36,6 @@ template <int D, bool PERM, int CT> struct TreeMath<bf16_t, D, PERM, CT> {
   static constexpr int PTERMS = 2;
   typedef uint32_t vrow_t __attribute__((ext_vector_type(EV / 2)));
   struct Row { bf16x8_t op[J]; };            // a column's operand: a query row
-  struct Feat { bf16x8_t hi[J], lo[J]; };    // phi of one, as two terms
   struct Weights { bf16x8_t t[PTERMS]; };    // probabilities of a set's keys, one column tile
   static __device__ __forceinline__ float to_log(float scale) { return scale * LOG2E; }
   static __device__ __forceinline__ float pexp(float x) { return fast_exp2(x); }
@@ -46,39 +45,54 @@ template <int D, bool PERM, int CT> struct TreeMath<bf16_t, D, PERM, CT> {
 #pragma unroll
     for (int j = 0; j < J; ++j) r.op[j] = *reinterpret_cast<const bf16x8_t*>(x + piece_feature<PERM>(j, q4));
   }
-  // phi, a piece at a time: with all of a row's exponentials at once the registers of the other operands do not hold
-  struct Stats { float m, z; };   // of a row: this lane's pieces and those of the lanes of the same r16
-  static __device__ __forceinline__ Stats stats_of(const Row& r, int phi) {
-    Stats t = {0.f, 1.f};
-    if (phi == PHI_SOFTMAX) {
-      float x[8];
-      t.m = -INFINITY;
+  // phi, a piece at a time: with all of a row's exponentials at once the registers of the other operands do not hold.
+  // (Of a row: this lane's pieces and those of the lanes of the same r16.)
+  struct Stats { float m, z; };
+  static __device__ __forceinline__ Stats softmax_stats(const Row& r) {
+    float x[8], m = -INFINITY, s = 0.f;
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        unpack_bf16x8(r.op[j], x);
+    for (int j = 0; j < J; ++j) {
+      unpack_bf16x8(r.op[j], x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) t.m = fmaxf(t.m, x[i]);
-      }
-      t.m = rows_max(t.m);
-      float s = 0.f;
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        unpack_bf16x8(r.op[j], x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += fast_exp2((x[i] - t.m) * LOG2E);
-      }
-      t.z = 1.f / rows_sum(s);
+      for (int i = 0; i < 8; ++i) m = fmaxf(m, x[i]);
     }
-    return t;
+    m = rows_max(m);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      unpack_bf16x8(r.op[j], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += fast_exp2((x[i] - m) * LOG2E);
+    }
+    return {m, 1.f / rows_sum(s)};
   }
-  static __device__ __forceinline__ void phi_piece(const Row& r, int j, Stats t, float (&x)[8], int phi) {
-    unpack_bf16x8(r.op[j], x);
+  // calls use(j, hi, lo) with piece j of phi(r) as two terms; the other maps' values are bf16 ones, which one term holds
+  template <typename F> static __device__ __forceinline__ void each_piece(const Row& r, int phi, F&& use) {
     if (phi == PHI_SOFTMAX) {
+      const Stats t = softmax_stats(r);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fast_exp2((x[i] - t.m) * LOG2E) * t.z;
-    } else if (phi == PHI_RELU) {
+      for (int j = 0; j < J; ++j) {
+        float x[8];
+        bf16x8_t hi, lo;
+        unpack_bf16x8(r.op[j], x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fmaxf(x[i], 0.f);
+        for (int i = 0; i < 8; ++i) x[i] = fast_exp2((x[i] - t.m) * LOG2E) * t.z;
+        two_terms(x, hi, lo);
+        use(j, hi, lo);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        bf16x8_t hi = r.op[j];
+        if (phi == PHI_RELU) {
+          float x[8];
+          unpack_bf16x8(hi, x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = fmaxf(x[i], 0.f);
+          hi = pack_bf16x8(x);
+        }
+        use(j, hi, __builtin_bit_cast(bf16x8_t, u32x4_t{0, 0, 0, 0}));
+      }
     }
   }
   static __device__ __forceinline__ void two_terms(float (&x)[8], bf16x8_t& hi, bf16x8_t& lo) {
@@ -89,17 +103,23 @@ template <int D, bool PERM, int CT> struct TreeMath<bf16_t, D, PERM, CT> {
     for (int i = 0; i < 8; ++i) t[i] = x[i] - t[i];
     lo = pack_bf16x8(t);
   }
-  // (phi and products of it pass through the tiles as two terms of 8 bits, with the product of the two second terms left out:
-  // 2^-16 of a value, far below the rounding of the output to bf16)
-  static __device__ __forceinline__ void feat_of(const Row& r, Feat& o, int phi) {
-    const Stats t = stats_of(r, phi);
+  // phi(q) of a wave's rows, in its own part of LDS: two terms of every piece, [piece][row tile][term][lane].  (phi and products of
+  // it pass through the tiles as two terms of 8 bits, with the product of the two second terms left out: 2^-16 of a value, far
+  // below the rounding of the output to bf16.)
+  static constexpr int FEAT_BYTES = J * CT * 2 * 1024;
+  static __device__ __forceinline__ void put_feat(const Row& r, unsigned char* lds, int ct, int lane, int phi) {
+    each_piece(r, phi, [&](int j, bf16x8_t hi, bf16x8_t lo) {
+      *reinterpret_cast<bf16x8_t*>(lds + ((j * CT + ct) * 2) * 1024 + 16 * lane) = hi;
+      *reinterpret_cast<bf16x8_t*>(lds + ((j * CT + ct) * 2 + 1) * 1024 + 16 * lane) = lo;
+    });
+  }
+  struct Piece { bf16x8_t hi[CT], lo[CT]; };
+  static __device__ __forceinline__ void get_feat(Piece& f, const unsigned char* lds, int j, int lane) {
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float x[8];
-      phi_piece(r, j, t, x, phi);
-      two_terms(x, o.hi[j], o.lo[j]);
+    for (int ct = 0; ct < CT; ++ct) {
+      f.hi[ct] = *reinterpret_cast<const bf16x8_t*>(lds + ((j * CT + ct) * 2) * 1024 + 16 * lane);
+      f.lo[ct] = *reinterpret_cast<const bf16x8_t*>(lds + ((j * CT + ct) * 2 + 1) * 1024 + 16 * lane);
     }
-    __builtin_amdgcn_sched_barrier(0);
   }
 
   // a set of rows in the tensors' type: keys at `stride` bytes
@@ -213,50 +233,45 @@ template <int D, bool PERM, int CT> struct TreeMath<bf16_t, D, PERM, CT> {
       for (int i = 0; i < 8; ++i) r[i] -= t[i];
     }
   }
-  // phi(k).phi(q) of keys 16c ..+15 of a set
-  static __device__ __forceinline__ void feature_scores(const Row& k, const Feat (&q)[CT], f32x4_t (&s)[CT][NT], int c, int phi) {
-    const Stats t = stats_of(k, phi);
+  // phi(k).phi(q) of 16 keys
+  static __device__ __forceinline__ void feature_scores(const Row& k, const unsigned char* lds, f32x4_t (&s)[CT], int lane, int phi) {
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) s[ct][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      float x[8];
-      bf16x8_t hi, lo;
-      phi_piece(k, j, t, x, phi);
-      two_terms(x, hi, lo);
+    for (int ct = 0; ct < CT; ++ct) s[ct] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    each_piece(k, phi, [&](int j, bf16x8_t hi, bf16x8_t lo) {
+      Piece f;
+      get_feat(f, lds, j, lane);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        s[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, q[ct].hi[j], s[ct][c], 0, 0, 0);
-        s[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[ct].lo[j], s[ct][c], 0, 0, 0);
-        s[ct][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[ct].hi[j], s[ct][c], 0, 0, 0);
+        s[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, f.hi[ct], s[ct], 0, 0, 0);
+        s[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, f.lo[ct], s[ct], 0, 0, 0);
+        s[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, f.hi[ct], s[ct], 0, 0, 0);
       }
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    });
   }
-  // piece j of the features: acc += S^T phi(q)^T over state rows piece_feature(j, q4) ..+7 of each lane group
+  // piece j of the features: acc += S^T phi(q)^T over state rows piece_feature(j, q4) ..+7 of each lane group, four of a lane's
+  // EV value features at a time
   struct State {
-    f32x4_t v[8][EV / 4];
-    __device__ __forceinline__ void load(const float* S, int j, int r16, int q4) {
+    static constexpr int PARTS = EV / 4;
+    f32x4_t v[PARTS][8];
+    __device__ __forceinline__ void load(const float* S, int j, int part, int r16, int q4) {
+      const float* s = S + (size_t)piece_feature<PERM>(j, q4) * D + EV * r16 + 4 * part;
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-#pragma unroll
-        for (int i = 0; i < EV / 4; ++i)
-          v[u][i] = *reinterpret_cast<const f32x4_t*>(S + (size_t)(piece_feature<PERM>(j, q4) + u) * D + EV * r16 + 4 * i);
+      for (int u = 0; u < 8; ++u) v[part][u] = *reinterpret_cast<const f32x4_t*>(s + u * D);
     }
-    __device__ __forceinline__ void accumulate(const Feat (&q)[CT], int j, f32x4_t (&acc)[CT][EV]) const {
+    __device__ __forceinline__ void accumulate(const Piece& f, int part, f32x4_t (&acc)[CT][EV]) const {
 #pragma unroll
-      for (int e = 0; e < EV; ++e) {
+      for (int e = 0; e < 4; ++e) {
         float x[8];
         bf16x8_t hi, lo;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = v[u][e >> 2][e & 3];
-        __builtin_amdgcn_sched_barrier(0);
+        for (int u = 0; u < 8; ++u) x[u] = v[part][u][e];
         two_terms(x, hi, lo);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          acc[ct][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, q[ct].hi[j], acc[ct][e], 0, 0, 0);
-          acc[ct][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[ct].lo[j], acc[ct][e], 0, 0, 0);
-          acc[ct][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, q[ct].hi[j], acc[ct][e], 0, 0, 0);
+          f32x4_t& a = acc[ct][4 * part + e];
+          a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, f.hi[ct], a, 0, 0, 0);
+          a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, f.lo[ct], a, 0, 0, 0);
+          a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, f.hi[ct], a, 0, 0, 0);
         }
       }
     }
@@ -268,7 +283,6 @@ template <int D, bool PERM, int CT> struct TreeMath<bf16_t, D, PERM, CT> {
 template <int D, bool PERM, int CT> struct TreeMath<float, D, PERM, CT> {
   static constexpr int KEYS = 16, EV = D / 16, NT = 1, J = D / 16;
   struct Row { f32x4_t op[J]; };   // features 16j + 4 q4 ..+3
-  typedef Row Feat;
   struct Weights { f32x4_t t; };
   static __device__ __forceinline__ f32x4_t mfma(float a, float b, f32x4_t c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ float to_log(float scale) { return scale; }
@@ -279,7 +293,7 @@ template <int D, bool PERM, int CT> struct TreeMath<float, D, PERM, CT> {
 #pragma unroll
     for (int j = 0; j < J; ++j) r.op[j] = *reinterpret_cast<const f32x4_t*>(x + 16 * j + 4 * q4);
   }
-  static __device__ __forceinline__ void feat_of(const Row& r, Feat& o, int phi) {
+  static __device__ __forceinline__ void feat_of(const Row& r, Row& o, int phi) {
     if (phi == PHI_SOFTMAX) {
       float m = -INFINITY, s = 0.f;
 #pragma unroll
@@ -300,6 +314,18 @@ template <int D, bool PERM, int CT> struct TreeMath<float, D, PERM, CT> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o.op[j][i] = phi == PHI_RELU ? fmaxf(r.op[j][i], 0.f) : r.op[j][i];
     }
+  }
+  static constexpr int FEAT_BYTES = J * CT * 1024;
+  static __device__ __forceinline__ void put_feat(const Row& r, unsigned char* lds, int ct, int lane, int phi) {
+    Row f;
+    feat_of(r, f, phi);
+#pragma unroll
+    for (int j = 0; j < J; ++j) *reinterpret_cast<f32x4_t*>(lds + (j * CT + ct) * 1024 + 16 * lane) = f.op[j];
+  }
+  struct Piece { f32x4_t x[CT]; };
+  static __device__ __forceinline__ void get_feat(Piece& f, const unsigned char* lds, int j, int lane) {
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) f.x[ct] = *reinterpret_cast<const f32x4_t*>(lds + (j * CT + ct) * 1024 + 16 * lane);
   }
   struct Base {
     Row k;
@@ -372,29 +398,31 @@ template <int D, bool PERM, int CT> struct TreeMath<float, D, PERM, CT> {
     }
   };
   static __device__ __forceinline__ void weights(const f32x4_t (&s)[NT], Weights& w) { w.t = s[0]; }
-  static __device__ __forceinline__ void feature_scores(const Row& k, const Feat (&q)[CT], f32x4_t (&s)[CT][NT], int, int phi) {
-    Feat f;
+  static __device__ __forceinline__ void feature_scores(const Row& k, const unsigned char* lds, f32x4_t (&s)[CT], int lane, int phi) {
+    Row f, q;
     feat_of(k, f, phi);
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) s[ct][0] = Base::dots(f, q[ct]);
+    for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) q.op[j] = *reinterpret_cast<const f32x4_t*>(lds + (j * CT + ct) * 1024 + 16 * lane);
+      s[ct] = Base::dots(f, q);
+    }
   }
   struct State {
-    f32x4_t v[4][D / 64];
-    __device__ __forceinline__ void load(const float* S, int j, int r16, int q4) {
+    static constexpr int PARTS = D / 64;
+    f32x4_t v[PARTS][4];
+    __device__ __forceinline__ void load(const float* S, int j, int part, int r16, int q4) {
+      const float* s = S + (size_t)(16 * j + 4 * q4) * D + 64 * part + 4 * r16;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int hf = 0; hf < D / 64; ++hf) v[i][hf] = *reinterpret_cast<const f32x4_t*>(S + (size_t)(16 * j + 4 * q4 + i) * D + 64 * hf + 4 * r16);
+      for (int i = 0; i < 4; ++i) v[part][i] = *reinterpret_cast<const f32x4_t*>(s + i * D);
     }
-    __device__ __forceinline__ void accumulate(const Feat (&q)[CT], int j, f32x4_t (&acc)[CT][EV]) const {
+    __device__ __forceinline__ void accumulate(const Piece& f, int part, f32x4_t (&acc)[CT][EV]) const {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int hf = 0; hf < D / 64; ++hf)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) acc[ct][4 * hf + e] = mfma(v[i][hf][e], q[ct].op[j][i], acc[ct][4 * hf + e]);
+          for (int ct = 0; ct < CT; ++ct) acc[ct][4 * part + e] = mfma(v[part][i][e], f.x[ct][i], acc[ct][4 * part + e]);
     }
   };
   static __device__ __forceinline__ int feature0(int e4, int i, int q4) { return 64 * e4 + 4 * (4 * q4 + i); }
@@ -527,13 +555,10 @@ __device__ __forceinline__ bool tree_row_out(const TreeArgs<IO, RT>& a, int n, i
 #pragma unroll
   for (int h = 0; h < NH; ++h) {
     const int d = 64 * h + 4 * r16;
-    f32x4_t y;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float g1 = a.gs ? a.gs[head * D + d + i] : 1.f, g2 = a.gr ? a.gr[head * D + d + i] : 1.f;
-      y[i] = g1 * xs[h][i] * r1 + g2 * xr[h][i] * r2;
-    }
-    store4(o + d, y);
+    f32x4_t g1 = {1.f, 1.f, 1.f, 1.f}, g2 = g1;
+    if (a.gs) __builtin_memcpy(&g1, a.gs + head * D + d, 16);   // (gains need no more than a float's alignment)
+    if (a.gr) __builtin_memcpy(&g2, a.gr + head * D + d, 16);
+    store4(o + d, g1 * xs[h] * r1 + g2 * xr[h] * r2);
   }
   return true;
 }
@@ -663,18 +688,7 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
         Math::weights(s[ct], pw[ct]);
       }
     };
-    int it = w0;
-    while (it < nring) {
-      const int base = ring_base(it);
-      it += nw;
-      const int next = it < nring ? ring_base(it) : 0;
-      f32x4_t s[CT][NT];
-      ring.scores(q, s);
-      if (it < nring) load_ring_k(next, nvalid - next);
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int c = 0; c < NT; ++c) s[ct][c] *= sc;
+    auto mask_ring = [&](f32x4_t (&s)[CT][NT], int base) {
       // ages in the set start at its first slot's, or at 0 where slot0 is inside
       const int youngest = base < slot0 && slot0 < base + KEYS ? 0 : age(base);
       if (base + KEYS > nvalid || youngest <= dmax) {   // wave-uniform
@@ -688,30 +702,74 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
             for (int ct = 0; ct < CT; ++ct) s[ct][c][i] = j > depth[ct] ? s[ct][c][i] : -INFINITY;
           }
       }
-      typename Math::Weights pw[CT];
-      softmax_step(s, pw);
-      ring.accumulate(pw, acc);
-      if (it < nring) load_ring_v(next, nvalid - next);
-    }
-    // drafted keys
-    for (; it < nset; it += nw) {
-      const int base = (it - nring) * KEYS;
-      NodeRows rows;
-      rows.load_k(node_rsrc(kn, base), nstride, r16, q4);
-      rows.load_v(node_rsrc(vn, base), nstride, r16, q4);
-      f32x4_t s[CT][NT];
-      rows.scores(q, s);
+    };
+    auto mask_nodes = [&](f32x4_t (&s)[CT][NT], int base) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         const unsigned see = (unsigned)(shfl64(node.anc & ~node.left, node_of[ct]) >> (base + 4 * q4));
 #pragma unroll
         for (int c = 0; c < NT; ++c)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[ct][c][i] = see >> (16 * c + i) & 1 ? s[ct][c][i] * sc : -INFINITY;
+          for (int i = 0; i < 4; ++i) s[ct][c][i] = see >> (16 * c + i) & 1 ? s[ct][c][i] : -INFINITY;
       }
+    };
+    // sets of ring keys (of rings in the tensors' type also of drafted keys, which come last)
+    const int nloop = PACKED ? nring : nset;
+    auto load_k = [&](int it) {
+      if constexpr (!PACKED) {
+        const bool r = it < nring;
+        const int base = r ? ring_base(it) : (it - nring) * KEYS;
+        ring.load_k(r ? make_rsrc(kr + (size_t)base * D, (unsigned)(min(KEYS, nvalid - base) * D * (int)sizeof(RT))) : node_rsrc(kn, base),
+                    r ? D * (int)sizeof(RT) : nstride, r16, q4);
+      } else load_ring_k(ring_base(it), nvalid - ring_base(it));
+    };
+    auto load_v = [&](int it) {
+      if constexpr (!PACKED) {
+        const bool r = it < nring;
+        const int base = r ? ring_base(it) : (it - nring) * KEYS;
+        ring.load_v(r ? make_rsrc(vr + (size_t)base * D, (unsigned)(min(KEYS, nvalid - base) * D * (int)sizeof(RT))) : node_rsrc(vn, base),
+                    r ? D * (int)sizeof(RT) : nstride, r16, q4);
+      } else load_ring_v(ring_base(it), nvalid - ring_base(it));
+    };
+    int it = w0;
+    if (PACKED || it < nring) {
+      // (requested in front of the tree's walk, above)
+    } else if (it < nloop) { load_k(it); load_v(it); }
+#pragma unroll 1
+    while (it < nloop) {
+      const int now = it;
+      it += nw;
+      f32x4_t s[CT][NT];
+      ring.scores(q, s);
+      if (it < nloop) load_k(it);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int c = 0; c < NT; ++c) s[ct][c] *= sc;
+      if (PACKED || now < nring) mask_ring(s, ring_base(now)); else mask_nodes(s, (now - nring) * KEYS);
       typename Math::Weights pw[CT];
       softmax_step(s, pw);
-      rows.accumulate(pw, acc);
+      ring.accumulate(pw, acc);
+      if (it < nloop) load_v(it);
+    }
+    if constexpr (PACKED) {
+#pragma unroll 1
+      for (; it < nset; it += nw) {
+        const int base = (it - nring) * KEYS;
+        NodeRows rows;
+        rows.load_k(node_rsrc(kn, base), nstride, r16, q4);
+        rows.load_v(node_rsrc(vn, base), nstride, r16, q4);
+        f32x4_t s[CT][NT];
+        rows.scores(q, s);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int c = 0; c < NT; ++c) s[ct][c] *= sc;
+        mask_nodes(s, base);
+        typename Math::Weights pw[CT];
+        softmax_step(s, pw);
+        rows.accumulate(pw, acc);
+      }
     }
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -724,71 +782,95 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
   } else {
     // ---- linear branch
     const int w0 = (kg - KW) * nsplit + sp, nw = (KG - KW) * nsplit;
-    typename Math::Feat f[CT];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) Math::feat_of(q[ct], f[ct], a.phi);
-    if (p > W) {
-      const float* S = a.state + (size_t)pair * D * D;
-#pragma unroll
-      for (int j = 0; j < Math::J; ++j)
-        if (j % nw == w0) {
-          typename Math::State st;
-          st.load(S, j, r16, q4);
-          st.accumulate(f, j, acc);
-        }
-    }
+    unsigned char* feats = reinterpret_cast<unsigned char*>(part + w * CT * 16 * LD);   // (free until the waves meet)
+    static_assert(Math::FEAT_BYTES <= CT * 16 * LD * 4, "features of a wave's rows");
     const TreeNodes node = tree_nodes(up, W, lane);
     depths(node);
-    // ring tokens that leave: slots slot0 .., then 0 ..; then drafted ones, where a path is longer than the window.  Of the waves the
-    // last come first (the first ones may have a piece of the state more)
+    // Keys that leave: ring tokens in slots slot0 .., then 0 ..; then drafted ones, where a path is longer than the window.  Of the
+    // waves the last come first (the first ones may have a piece of the state more)
     const bool any = p + dmax >= W;
     const int nleave = any ? min(dmax + 1, W) : 0, len0 = min(nleave, W - slot0), sets0 = (len0 + KEYS - 1) / KEYS;
     const int sets = sets0 + (nleave - len0 + KEYS - 1) / KEYS, nodes = any && dmax >= W ? (cnt + KEYS - 1) / KEYS : 0;
-    for (int x = nw - 1 - w0; x < sets + nodes; x += nw) {
-      f32x4_t s[CT][NT];
-      typename Math::Weights pw[CT];
-      if (x < sets) {
-        const int base = x < sets0 ? slot0 + x * KEYS : (x - sets0) * KEYS;
-        const int rows = min(KEYS, min(x < sets0 ? slot0 + len0 : nleave - len0, nvalid) - base);
-        if (rows <= 0) continue;   // (a ring that is not full: those slots hold nothing yet)
-        load_ring_k(base, rows);
-        load_ring_v(base, rows);
+    auto leave_base = [&](int x) { return x < sets0 ? slot0 + x * KEYS : (x - sets0) * KEYS; };
+    auto leave_rows = [&](int x) {   // (a ring that is not full: the first of those slots hold nothing yet)
+      return min(KEYS, min(x < sets0 ? slot0 + len0 : nleave - len0, nvalid) - leave_base(x));
+    };
+    auto load_leaving = [&](int x) {
+      if (x < sets && leave_rows(x) > 0) {
+        load_ring_k(leave_base(x), leave_rows(x));
+        load_ring_v(leave_base(x), leave_rows(x));
+      }
+    };
+    int x = nw - 1 - w0;
+    load_leaving(x);
+    if (any) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) Math::put_feat(q[ct], feats, ct, lane, a.phi);
+    }
+#pragma unroll 1
+    for (; x < sets; x += nw) {
+      const int base = leave_base(x), rows = leave_rows(x);
+      if (rows > 0) {
+        f32x4_t s[CT][NT];
 #pragma unroll
         for (int c = 0; c < NT; ++c) {
           typename Math::Row kx;
           ring.key_row(c, kx);
-          Math::feature_scores(kx, f, s, c, a.phi);
+          f32x4_t t[CT];
+          Math::feature_scores(kx, feats, t, lane, a.phi);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int r = 16 * c + 4 * q4 + i, j = r < rows ? age(base + r) : W;
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) s[ct][c][i] = j <= depth[ct] && j < W ? s[ct][c][i] : 0.f;
+            for (int ct = 0; ct < CT; ++ct) s[ct][c][i] = j <= depth[ct] && j < W ? t[ct][i] : 0.f;
           }
         }
+        typename Math::Weights pw[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) Math::weights(s[ct], pw[ct]);
         ring.accumulate(pw, acc);
-      } else {
-        const int base = (x - sets) * KEYS;
-        NodeRows rows;
-        rows.load_k(node_rsrc(kn, base), nstride, r16, q4);
-        rows.load_v(node_rsrc(vn, base), nstride, r16, q4);
+      }
+      load_leaving(x + nw);
+    }
+#pragma unroll 1
+    for (; x < sets + nodes; x += nw) {
+      const int base = (x - sets) * KEYS;
+      NodeRows rows;
+      rows.load_k(node_rsrc(kn, base), nstride, r16, q4);
+      rows.load_v(node_rsrc(vn, base), nstride, r16, q4);
+      f32x4_t s[CT][NT];
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-          typename Math::Row kx;
-          rows.key_row(c, kx);
-          Math::feature_scores(kx, f, s, c, a.phi);
-        }
+      for (int c = 0; c < NT; ++c) {
+        typename Math::Row kx;
+        rows.key_row(c, kx);
+        f32x4_t t[CT];
+        Math::feature_scores(kx, feats, t, lane, a.phi);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           const unsigned see = (unsigned)(shfl64(node.left, node_of[ct]) >> (base + 4 * q4));
 #pragma unroll
-          for (int c = 0; c < NT; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[ct][c][i] = see >> (16 * c + i) & 1 ? s[ct][c][i] : 0.f;
-          Math::weights(s[ct], pw[ct]);
+          for (int i = 0; i < 4; ++i) s[ct][c][i] = see >> (16 * c + i) & 1 ? t[ct][i] : 0.f;
         }
-        rows.accumulate(pw, acc);
+      }
+      typename Math::Weights pw[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) Math::weights(s[ct], pw[ct]);
+      rows.accumulate(pw, acc);
+    }
+    // pieces of the state, each part of the next one under way when this one's products are done
+    if (p > W && w0 < Math::J) {
+      const float* S = a.state + (size_t)pair * D * D;
+      typename Math::State st;
+#pragma unroll
+      for (int h = 0; h < Math::State::PARTS; ++h) st.load(S, w0, h, r16, q4);
+      for (int j = w0; j < Math::J; j += nw) {
+        typename Math::Piece f;
+        Math::get_feat(f, feats, j, lane);
+#pragma unroll
+        for (int h = 0; h < Math::State::PARTS; ++h) {
+          st.accumulate(f, h, acc);
+          if (j + nw < Math::J) st.load(S, j + nw, h, r16, q4);
+        }
       }
     }
   }
@@ -806,99 +888,100 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
   const int group = w * 4 + q4;
   auto turn_row = [&](int turn) { return turn * 4 * NW + group; };
   auto slice = [&](int t, int k) { return (k * RG + t / (16 * CT)) * 16 * CT + t % (16 * CT); };
-  f32x4_t xs[TURNS][NH], xr[TURNS][NH];
-  float top[TURNS], den[TURNS];
-#pragma unroll
-  for (int turn = 0; turn < TURNS; ++turn) {
+  f32x4_t xs[NH], xr[NH];
+  float top, den;
+  auto add_up = [&](int turn) {
     const int t = min(turn_row(turn), ROWS - 1);
-    top[turn] = -1.0e30f;
-    den[turn] = 0.f;
+    top = -1.0e30f;
+    den = 0.f;
 #pragma unroll
-    for (int h = 0; h < NH; ++h) xs[turn][h] = xr[turn][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < KG; ++k)
-      if (k < KW) top[turn] = fmaxf(top[turn], ml[slice(t, k) * 2]);
+    for (int h = 0; h < NH; ++h) xs[h] = xr[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // (a factor for either branch: what is no finite number in one of them is looked at again in both anyway)
+    float mk[KG], lk[KG];
 #pragma unroll
     for (int k = 0; k < KG; ++k) {
-      f32x4_t x[NH];
+      mk[k] = ml[slice(t, k) * 2];
+      lk[k] = ml[slice(t, k) * 2 + 1];
+      top = fmaxf(top, k < KW ? mk[k] : top);
+    }
 #pragma unroll
-      for (int h = 0; h < NH; ++h) x[h] = *reinterpret_cast<const f32x4_t*>(part + slice(t, k) * LD + 64 * h + 4 * r16);
-      if (k < KW) {
-        const float f = Math::pexp(ml[slice(t, k) * 2] - top[turn]);
-        den[turn] = __builtin_fmaf(f, ml[slice(t, k) * 2 + 1], den[turn]);
+    for (int k = 0; k < KG; ++k) {
+      const float f = k < KW ? Math::pexp(mk[k] - top) : 0.f, add = k < KW ? 0.f : 1.f;
+      den += k < KW ? f * lk[k] : 0.f;
 #pragma unroll
-        for (int h = 0; h < NH; ++h) xs[turn][h] += f * x[h];
-      } else {
-#pragma unroll
-        for (int h = 0; h < NH; ++h) xr[turn][h] += x[h];
+      for (int h = 0; h < NH; ++h) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(part + slice(t, k) * LD + 64 * h + 4 * r16);
+        xs[h] += f * x;
+        xr[h] += add * x;
       }
     }
-  }
-  // ---- SPLIT: the sums of all work-groups of these rows, by the one that arrives last (see SplitArgs)
-  if constexpr (SPLIT) {
-    constexpr int LINE = SplitArgs::row(D);
+  };
+  unsigned again = 0;   // turns whose row has something that is no finite number
+  auto out = [&](int turn) {
+    const int t = turn_row(turn);
+    if (!tree_row_out<IO, RT, D>(a, n, g, row0 + t, r16, xs, xr, den, t < ROWS && row0 + t < nrows)) again |= 1u << turn;
+  };
+  if constexpr (!SPLIT) {
+#pragma unroll 1
+    for (int turn = 0; turn < TURNS; ++turn) { add_up(turn); out(turn); }
+  } else {
+    // the sums of all work-groups of these rows, by the one that arrives last (see SplitArgs)
+    constexpr int LINE = SplitArgs::row(D), AT_ONCE = 4;
     const size_t cell = (size_t)pair * a.blocks + block;
-    float* all = split.part + cell * split.n * ROWS * LINE;
-    const rsrc_t mem = make_rsrc(all, (unsigned)(split.n * ROWS * LINE * 4));
-#pragma unroll
+    const rsrc_t mem = make_rsrc(split.part + cell * split.n * ROWS * LINE, (unsigned)(split.n * ROWS * LINE * 4));
+#pragma unroll 1
     for (int turn = 0; turn < TURNS; ++turn) {
-      const int t = turn_row(turn);
-      if (t < ROWS && row0 + t < nrows) {
-        const int at = (sp * ROWS + t) * LINE * 4;
+      const int t = turn_row(turn), at = (sp * ROWS + t) * LINE * 4;
+      add_up(turn);
+      if (t >= ROWS || row0 + t >= nrows) continue;
 #pragma unroll
-        for (int h = 0; h < NH; ++h) {
-          put_shared16(mem, xs[turn][h], at + 256 * h + 16 * r16);
-          put_shared16(mem, xr[turn][h], at + 4 * D + 256 * h + 16 * r16);
-        }
-        if (r16 == 0) put_shared16(mem, f32x4_t{top[turn], den[turn], 0.f, 0.f}, at + 8 * D);
+      for (int h = 0; h < NH; ++h) {
+        put_shared16(mem, xs[h], at + 256 * h + 16 * r16);
+        put_shared16(mem, xr[h], at + 4 * D + 256 * h + 16 * r16);
       }
+      if (r16 == 0) put_shared16(mem, f32x4_t{top, den, 0.f, 0.f}, at + 8 * D);
     }
     if (!arrive_last(split.ticket + cell, split.nonce, nsplit)) return;
-    constexpr int AT_ONCE = 4;
-#pragma unroll
+#pragma unroll 1
     for (int turn = 0; turn < TURNS; ++turn) {
       const int t = turn_row(turn);
-      if (t >= ROWS || row0 + t >= nrows) continue;
-      top[turn] = -1.0e30f;
-      den[turn] = 0.f;
+      top = -1.0e30f;
+      den = 0.f;
 #pragma unroll
-      for (int h = 0; h < NH; ++h) xs[turn][h] = xr[turn][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      for (int k0 = 0; k0 < nsplit; k0 += AT_ONCE) {
-        f32x4_t x[AT_ONCE][NH], y[AT_ONCE][NH], ml4[AT_ONCE];
+      for (int h = 0; h < NH; ++h) xs[h] = xr[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if (t < ROWS && row0 + t < nrows)
+#pragma unroll 1
+        for (int k0 = 0; k0 < nsplit; k0 += AT_ONCE) {
+          f32x4_t x[AT_ONCE][NH], y[AT_ONCE][NH], md[AT_ONCE];
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) {
-          const int at = (min(k0 + k, nsplit - 1) * ROWS + t) * LINE * 4;
-          ml4[k] = get_shared16(mem, at + 8 * D);
+          for (int k = 0; k < AT_ONCE; ++k) {
+            const int at = (min(k0 + k, nsplit - 1) * ROWS + t) * LINE * 4;
+            md[k] = get_shared16(mem, at + 8 * D);
 #pragma unroll
-          for (int h = 0; h < NH; ++h) {
-            x[k][h] = get_shared16(mem, at + 256 * h + 16 * r16);
-            y[k][h] = get_shared16(mem, at + 4 * D + 256 * h + 16 * r16);
+            for (int h = 0; h < NH; ++h) {
+              x[k][h] = get_shared16(mem, at + 256 * h + 16 * r16);
+              y[k][h] = get_shared16(mem, at + 4 * D + 256 * h + 16 * r16);
+            }
           }
+          float to = top;
+#pragma unroll
+          for (int k = 0; k < AT_ONCE; ++k) to = fmaxf(to, md[k][0]);
+          const float keep = Math::pexp(top - to);
+          top = to;
+          den *= keep;
+#pragma unroll
+          for (int h = 0; h < NH; ++h) xs[h] *= keep;
+#pragma unroll
+          for (int k = 0; k < AT_ONCE; ++k)
+            if (k0 + k < nsplit) {
+              const float f = Math::pexp(md[k][0] - to);
+              den += f * md[k][1];
+#pragma unroll
+              for (int h = 0; h < NH; ++h) { xs[h] += f * x[k][h]; xr[h] += y[k][h]; }
+            }
         }
-        float to = top[turn];
-#pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) to = fmaxf(to, ml4[k][0]);
-        const float keep = Math::pexp(top[turn] - to);
-        top[turn] = to;
-        den[turn] *= keep;
-#pragma unroll
-        for (int h = 0; h < NH; ++h) xs[turn][h] *= keep;
-#pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k)
-          if (k0 + k < nsplit) {
-            const float f = Math::pexp(ml4[k][0] - to);
-            den[turn] += f * ml4[k][1];
-#pragma unroll
-            for (int h = 0; h < NH; ++h) { xs[turn][h] += f * x[k][h]; xr[turn][h] += y[k][h]; }
-          }
-      }
+      out(turn);
     }
-  }
-  unsigned again = 0;   // turns whose row has something that is no finite number
-#pragma unroll
-  for (int turn = 0; turn < TURNS; ++turn) {
-    const int t = turn_row(turn);
-    if (!tree_row_out<IO, RT, D>(a, n, g, row0 + t, r16, xs[turn], xr[turn], den[turn], t < ROWS && row0 + t < nrows)) again |= 1u << turn;
   }
   if (!__any(again != 0)) return;
   const TreeNodes node = tree_nodes(up, W, lane);
