@@ -420,6 +420,32 @@ def _on_device(dev, **tensors):
         raise ValueError(f"the tensors are on {dev}, which is not the current device")
 
 
+def _no_native(*args):
+    return None
+
+
+# The native marshalling of these calls (see _marshal): the result, None where the arguments are left to the Python path below, a
+# status.  Where it has not been built for this torch all are.
+class _Native:
+    def __getattr__(self, name):   # until the first call
+        L = lib()
+        try:
+            from . import _marshal
+        except ImportError:
+            names = dict.fromkeys(("ring_pack", "ring_unpack", "decode_step_packed", "tree_step", "tree_commit"), _no_native)
+        else:
+            addr = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+            _marshal.bind_cache(addr(L.rattn_ring_pack), addr(L.rattn_ring_unpack), addr(L.rattn_decode_packed_workspace_bytes),
+                                addr(L.rattn_decode_step_packed), addr(L.rattn_tree_workspace_bytes), addr(L.rattn_tree_step),
+                                addr(L.rattn_tree_commit))
+            names = {n: getattr(_marshal, n) for n in ("ring_pack", "ring_unpack", "decode_step_packed", "tree_step", "tree_commit")}
+        self.__dict__.update(names)
+        return names[name]
+
+
+_native = _Native()
+
+
 def _check_packed(N, Hkv, W, D, k_codes, k_scale, v_codes, v_scale):
     for name, t, dt, n in (("k_codes", k_codes, 0, D), ("k_scale", k_scale, 1, D // 32), ("v_codes", v_codes, 0, D),
                            ("v_scale", v_scale, 1, D // 32)):
@@ -436,6 +462,11 @@ def _ring_plan(shape, dtype):
 def rattn_ring_pack(k_ring, v_ring, out=None):
     """Rings [N,Hkv,W,D] in 8 bits: (k_codes, k_scale, v_codes, v_scale), codes float8_e4m3fn [N,Hkv,W,D] and scales
     float8_e8m0fnu [N,Hkv,W,D/32]; a feature is its code times the scale of its 32 features.  `out`: those four, to be reused."""
+    r = _native.ring_pack(k_ring, v_ring, out)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r)
+        return r
     if k_ring.dim() != 4 or v_ring.shape != k_ring.shape or k_ring.dtype not in _DTYPES or v_ring.dtype != k_ring.dtype:
         raise ValueError("k_ring and v_ring must share shape [N,Hkv,W,D] and dtype float32 or bfloat16")
     N, Hkv, W, D = k_ring.shape
@@ -455,8 +486,16 @@ def rattn_ring_unpack(k_codes, k_scale, v_codes, v_scale, dtype=torch.bfloat16, 
     if k_codes.dim() != 4 or dtype not in _DTYPES:
         raise ValueError("codes must be [N,Hkv,W,D] and dtype float32 or bfloat16")
     shape = k_codes.shape
+    if out is None:
+        out = tuple(torch.empty(shape, dtype=dtype, device=k_codes.device) for _ in range(2))
+    kr, vr = out
+    if kr.dtype == dtype:
+        r = _native.ring_unpack(k_codes, k_scale, v_codes, v_scale, out)
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return r
     _check_packed(*shape, k_codes, k_scale, v_codes, v_scale)
-    kr, vr = (torch.empty(shape, dtype=dtype, device=k_codes.device) for _ in range(2)) if out is None else out
     if kr.shape != shape or vr.shape != shape or kr.dtype != dtype or vr.dtype != dtype:
         raise ValueError("out must be two rings of the codes' shape in `dtype`")
     _on_device(k_codes.device, k_codes=k_codes, k_scale=k_scale, v_codes=v_codes, v_scale=v_scale, k_ring=kr, v_ring=vr)
@@ -483,6 +522,12 @@ def _check_out(out, q):
 def rattn_decode_step_packed(q, k_new, v_new, pos, k_codes, k_scale, v_codes, v_scale, state, gamma_swa=None, gamma_rla=None,
                              softmax_scale=1.0, rms_eps=1e-6, out=None, feature_map="softmax"):
     """rattn_decode_step over packed rings (see rattn_ring_pack), which are updated in place as the state is; returns o [N,Hq,D]."""
+    o = _native.decode_step_packed(q, k_new, v_new, pos, k_codes, k_scale, v_codes, v_scale, state, gamma_swa, gamma_rla,
+                                   softmax_scale, rms_eps, out, feature_map)
+    if o is not None:
+        if o.__class__ is int:
+            _check(o)
+        return o
     N, Hq, D = q.shape
     Hkv, W = k_codes.shape[1:3]
     _on_device(q.device, q=q, k_new=k_new, v_new=v_new, pos=pos, k_codes=k_codes, k_scale=k_scale, v_codes=v_codes, v_scale=v_scale,
@@ -546,6 +591,12 @@ def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None,
     q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M]: the earlier node that a node continues, -1 = the sequence's last token;
     pos int32 [N]: tokens in the cache; count int32 [N]: nodes of each sequence (None: M), rows behind them are left as they are
     in `out` (zero where it is allocated here).  k_scale, v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
+    o = _native.tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa, gamma_rla, softmax_scale, rms_eps, count, k_scale,
+                          v_scale, out, feature_map)
+    if o is not None:
+        if o.__class__ is int:
+            _check(o)
+        return o
     if q.dim() != 4 or q.dtype != k.dtype or k.dim() != 4 or (q.shape[0], q.shape[1], q.shape[3]) != (k.shape[0], k.shape[1], k.shape[3]):
         raise ValueError("q must be [N,M,Hq,D] like k and v [N,M,Hkv,D], in their dtype")
     W = _check_tree(k, v, parent, pos, k_ring, v_ring, state, k_scale, v_scale, q=q, count=count)
@@ -566,6 +617,11 @@ def rattn_tree_commit(k, v, parent, accepted, pos, k_ring, v_ring, state, k_scal
     """The accepted node of each sequence's tree and its ancestors become tokens of the cache: rings (packed where scales are
     given) and state are updated in place.  accepted int32 [N]: node, or -1 for none.  pos is left to the caller, who advances it by
     the length of the accepted path when every layer is done."""
+    r = _native.tree_commit(k, v, parent, accepted, pos, k_ring, v_ring, state, k_scale, v_scale, feature_map)
+    if r is not None:
+        if r.__class__ is int:
+            _check(r)
+        return
     W = _check_tree(k, v, parent, pos, k_ring, v_ring, state, k_scale, v_scale, accepted=accepted)
     p, _ = _tree_plan(k.shape, k.shape[2], W, k.dtype, k_scale is not None, 1.0, 1e-6, feature_map)
     _check(lib().rattn_tree_commit(p, _ptr(k), _ptr(v), _ptr(parent), _ptr(accepted), _ptr(pos), _ptr(k_ring), _ptr(k_scale),
