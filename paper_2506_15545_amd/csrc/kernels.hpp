@@ -250,11 +250,13 @@ struct TreeTensors {
 };
 // How a tree step is cut: a work-group of NW waves has (NW / KG) groups of 16 CT rows (a row is a query head of a node; the rows of a
 // (sequence, KV head) are its nodes' heads in order), each shared by KG waves that divide the keys, KW of them those of the softmax
-// branch; `blocks` work-groups for all rows of a pair, and `nsplit` for the keys of each.
+// branch; `blocks` work-groups for all rows of a pair, and `nsplit` for the keys of each.  With `tiles` (many rows, tree_tiles.hpp) a
+// wave has 32 rows to itself: CT = 2, KG = 1.
 struct TreePlan {
-  int CT, KG, NW, blocks, nsplit, KW;
+  int CT, KG, NW, blocks, nsplit, KW, tiles;
   size_t part_off, bytes;   // workspace: tickets from offset 0 (nothing: 0 bytes)
 };
+constexpr int TREE_TILE_MIN_WAVES = 4;   // of a work-group with `tiles`
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed);
 void tree_step(const TreeDims& td, int dtype, const TreeTensors& t, hipStream_t st);
 void tree_commit(const TreeDims& td, int dtype, const TreeTensors& t, const int32_t* accepted, hipStream_t st);

@@ -147,8 +147,29 @@ ExportPlan export_plan(const LayerDims& dm) {
 }
 
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
-  TreePlan p = {1, 8, 8, 1, 1, 6, 0, 0};
+  TreePlan p = {1, 8, 8, 1, 1, 6, 0, 0, 0};
   const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32;
+  const long long pairs = (long long)td.N * td.Hkv;
+  auto workspace = [&](int per) {
+    const long long groups = pairs * p.blocks;
+    if (p.nsplit > 1) {
+      p.part_off = ((size_t)groups * 8 + 255) / 256 * 256;
+      p.bytes = p.part_off + (size_t)groups * p.nsplit * per * (2 * td.D + 4) * 4;
+    }
+    return p;
+  };
+  if (dtype == 1 && rows > 64) {
+    const int t32 = (rows + 31) / 32;
+    p.tiles = 1;
+    p.CT = 2;
+    p.KG = 1;
+    p.blocks = (t32 + 3) / 4;
+    p.NW = 4;
+    const int tiles = (td.W + 63) / 64 + 1;
+    p.nsplit = DEC_MAX_SPLIT;
+    while (p.nsplit > 1 && (pairs * p.blocks * p.nsplit > 256 || tiles < 2 * p.nsplit)) p.nsplit /= 2;
+    return workspace(32 * p.NW);
+  }
   if (dtype == 0) {
     p.KG = rows <= 16 ? 8 : 4;
   } else if (rows > 16) {
@@ -156,7 +177,6 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
     p.KG = rows <= 32 ? 8 : 4;
   }
   const int group = 16 * p.CT;
-  const long long pairs = (long long)td.N * td.Hkv;
   if (rows <= group && pairs >= 256) p.KG = p.NW = 4;
   const int per = p.NW / p.KG * group;
   p.blocks = (rows + per - 1) / per;
@@ -169,11 +189,7 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   p.KW = p.KG - kl;
   p.nsplit = DEC_MAX_SPLIT;
   while (p.nsplit > 1 && (groups * p.nsplit > 256 || sets < p.KW * p.nsplit)) p.nsplit /= 2;
-  if (p.nsplit > 1) {
-    p.part_off = ((size_t)groups * 8 + 255) / 256 * 256;
-    p.bytes = p.part_off + (size_t)groups * p.nsplit * per * (2 * td.D + 4) * 4;
-  }
-  return p;
+  return workspace(per);
 }
 
 }  // namespace rattn

@@ -616,8 +616,8 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
     if constexpr (PACKED) ring.load_v(r, make_rsrc(vrs + (size_t)base * SB, (unsigned)(rows * SB)), r16, q4);
     else ring.load_v(r, D * (int)sizeof(RT), r16, q4);
   };
-  auto node_rsrc = [&](const IO* x, int base) {   // nodes base .. M-1 of this sequence (of the last one only its D features)
-    return make_rsrc(x + (size_t)base * Hkv * D, (unsigned)((M - 1 - base) * nstride + D * (int)sizeof(IO)));
+  auto node_rsrc = [&](const IO* x, int base) {   // nodes base .. cnt-1 of this sequence (of the last one only its D features)
+    return make_rsrc(x + (size_t)base * Hkv * D, (unsigned)((cnt - 1 - base) * nstride + D * (int)sizeof(IO)));
   };
   // age of the token in a slot
   auto age = [&](int slot) { return slot - slot0 + (slot < slot0 ? W : 0); };
@@ -996,15 +996,19 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
   }
 }
 
+template <typename IO, typename RT> TreeArgs<IO, RT> tree_args(const TreeDims& td, const TreeTensors& t, const TreePlan& pl) {
+  return {(const IO*)t.q, (const IO*)t.k, (const IO*)t.v, t.parent, t.count, t.pos, (const RT*)t.k_ring, (const RT*)t.v_ring,
+          (const float*)t.state, t.gs, t.gr, (IO*)t.o, td.N, td.M, td.Hq, td.Hkv, td.W, td.G, pl.blocks, td.phi, td.scale, td.eps,
+          (const uint8_t*)t.k_scale, (const uint8_t*)t.v_scale};
+}
+
 template <typename IO, typename RT, int D, int CT, int KG, int NW, bool SPLIT>
 void launch_tree(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
   const size_t bytes = tree_lds_bytes(D, CT, NW);
   static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void*>(tree_kernel<IO, RT, D, CT, KG, NW, SPLIT>),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
   (void)attr;
-  const TreeArgs<IO, RT> a = {(const IO*)t.q, (const IO*)t.k, (const IO*)t.v, t.parent, t.count, t.pos, (const RT*)t.k_ring,
-                              (const RT*)t.v_ring, (const float*)t.state, t.gs, t.gr, (IO*)t.o, td.N, td.M, td.Hq, td.Hkv, td.W,
-                              td.G, pl.blocks, td.phi, td.scale, td.eps, (const uint8_t*)t.k_scale, (const uint8_t*)t.v_scale};
+  const TreeArgs<IO, RT> a = tree_args<IO, RT>(td, t, pl);
   std::conditional_t<SPLIT, SplitArgs, NoSplit> split;
   if constexpr (SPLIT)
     split = {(float*)((char*)td.workspace + pl.part_off), (unsigned long long*)td.workspace, td.nonce, pl.nsplit, 0};

@@ -1,0 +1,556 @@
+// Tree steps of many rows (bf16; see tree_group.hpp for the mathematics): the keys come through LDS, where the waves of a work-group
+// share them, each for 32 rows of its own.
+//
+// Few rows are bound by what a CU takes in; with many every wave would fetch the same ring again (192 pairs, W = 2048, 230 rows each:
+// 2 GB through L1 at 64 bytes a cycle and CU), so here a tile of 64 keys is fetched once for up to 256 rows.  The formulation is the
+// layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
+// second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
+// phi(k) of the keys that leave, then the state, both as two bf16 terms.
+#pragma once
+#include "tree_group.hpp"
+
+namespace rattn {
+
+namespace {
+
+constexpr int TILE_KEYS = 64;
+static_assert(TREE_TILE_MIN_WAVES == 4, "packed pieces of a tile that a thread has on the way");
+template <int D> constexpr size_t tree_tile_lds() { return 4 * (size_t)TileGeom<D>::KT; }   // two buffers of a K and a V tile
+
+// 16 bytes of a tile: chunk c (8 features) of row r
+template <int D> __device__ __forceinline__ unsigned char* tile_chunk(unsigned char* tile, int r, int c) {
+  return tile + r * TileGeom<D>::ROWB + ((c ^ swz<D>(r)) << 4);
+}
+// lds_row, lds_trp and lds_trn (mfma.hpp) of tiles whose address is known to lie in LDS: which of two buffers it is changes from
+// tile to tile, and through a general pointer the compiler would ask where it points
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+// 1024 bytes of a tile (block b: rows RPB b ..) straight from memory; rows from nrows on are read as row nrows - 1
+template <int D> __device__ __forceinline__ void tile_block(const uint16_t* rows, size_t stride, int nrows, lds_byte* tile, int b, int lane) {
+  typedef TileGeom<D> G;
+  const int r = b * G::RPB + lane / G::CH, c = (lane % G::CH) ^ swz<D>(r);
+  dma16(rows + (size_t)min(r, nrows - 1) * stride + c * 8, (unsigned)(size_t)(tile + b * 1024));
+}
+template <int D> __device__ __forceinline__ bf16x8_t tile_row(const lds_byte* tile, const LaneOff<D>& lo, int R0, int c2) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8_t*>(tile + lo.row[c2] + R0 * TileGeom<D>::ROWB);
+}
+__device__ __forceinline__ bf16x8_t tile_tr2(const lds_byte* pa, const lds_byte* pb) {
+  union { struct { s16x4_t lo, hi; } s; bf16x8_t v; } u;
+  u.s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(pa));
+  u.s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)(pb));
+  return u.v;
+}
+template <int D> __device__ __forceinline__ bf16x8_t tile_trp(const lds_byte* tile, const LaneOff<D>& lo, int K0, int ct) {
+  return tile_tr2(tile + lo.trp[ct][0] + K0 * TileGeom<D>::ROWB, tile + lo.trp[ct][1] + K0 * TileGeom<D>::ROWB);
+}
+template <int D> __device__ __forceinline__ bf16x8_t tile_trn(const lds_byte* tile, const LaneOffN<D>& lo, int K0, int ct) {
+  return tile_tr2(tile + lo.trn[ct][0] + K0 * TileGeom<D>::ROWB, tile + lo.trn[ct][1] + K0 * TileGeom<D>::ROWB);
+}
+template <int LANES> __device__ __forceinline__ float lanes_max(float x) {
+  x = fmaxf(x, dpp_get<0xB1>(x));
+  x = fmaxf(x, dpp_get<0x4E>(x));
+  x = fmaxf(x, dpp_get<0x141>(x));
+  return LANES == 16 ? fmaxf(x, dpp_get<0x140>(x)) : x;
+}
+template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
+  x += dpp_get<0xB1>(x);
+  x += dpp_get<0x4E>(x);
+  x += dpp_get<0x141>(x);
+  return LANES == 16 ? x + dpp_get<0x140>(x) : x;
+}
+__device__ __forceinline__ void split2(float (&x)[8], bf16x8_t& hi, bf16x8_t& lo) {   // (see TreeMath::two_terms)
+  float t[8];
+  hi = pack_bf16x8(x);
+  unpack_bf16x8(hi, t);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = x[i] - t[i];
+  lo = pack_bf16x8(t);
+}
+
+template <typename RT, int D, bool SPLIT>
+__global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> a, std::conditional_t<SPLIT, SplitArgs, NoSplit> split) {
+  constexpr bool PACKED = sizeof(RT) == 1;
+  typedef TileGeom<D> TG;
+  constexpr int KT = TG::KT, CH = TG::CH, SB = scale_bytes(D), NCT = D / 32, NC2 = D / 16;
+  extern __shared__ __align__(16) unsigned char smem[];   // [2][K, V][64 rows]
+  const int lane = lane_id(), w = wave_id(), nwave = blockDim.x >> 6, r32 = lane & 31, hl = lane >> 5;
+  const int W = a.W, G = a.G, M = a.M, Hkv = a.Hkv, rows_wg = 32 * nwave;
+  const unsigned pairs = a.N * Hkv, per = (pairs + 7) / 8 * 8 * a.blocks;   // (as in tree_kernel)
+  const int sp = SPLIT ? blockIdx.x / per : 0;
+  const unsigned id = SPLIT ? blockIdx.x % per : blockIdx.x;
+  const unsigned pair = id / (8 * a.blocks) * 8 + id % 8;
+  const int block = id / 8 % a.blocks;
+  if (pair >= pairs) return;
+  const int g = pair % Hkv, n = pair / Hkv;
+  const int p = a.pos[n], cnt = a.count ? min(a.count[n], M) : M;
+  const int row0 = block * rows_wg, nrows = cnt * G;
+  if (row0 >= nrows || p < 0) return;
+  const int nsplit = SPLIT ? split.n : 1;
+  const int slot0 = p % W, nvalid = min(p, W);
+  const RT *kr = a.k_ring + (size_t)pair * W * D, *vr = a.v_ring + (size_t)pair * W * D;
+  const uint8_t* krs = PACKED ? a.ks + (size_t)pair * W * SB : nullptr;
+  const uint8_t* vrs = PACKED ? a.vs + (size_t)pair * W * SB : nullptr;
+  const bf16_t *kn = a.k + ((size_t)n * M * Hkv + g) * D, *vn = a.v + ((size_t)n * M * Hkv + g) * D;
+  const size_t nstride = (size_t)Hkv * D;
+  auto age = [&](int slot) { return slot - slot0 + (slot < slot0 ? W : 0); };
+
+  // ---- this wave's rows: lane r32 has row r32's operand, features 16 c2 + 8 hl ..+7.  A negative scale goes to q's signs, so
+  // that the largest score is that of the largest product
+  const int up = lane < M ? a.parent[(size_t)n * M + lane] : -1;
+  const int row = min(row0 + 32 * w + r32, nrows - 1), node_of = row / G;
+  const bool live = row0 + 32 * w < nrows;   // (of the wave: the last work-group of a pair may have rows for some of its waves only)
+  bf16x8_t q[NC2];
+  {
+    const bf16_t* qp = a.q + (((size_t)n * M + node_of) * a.Hq + g * G + row % G) * D + 8 * hl;
+#pragma unroll
+    for (int c2 = 0; c2 < NC2; ++c2) q[c2] = *reinterpret_cast<const bf16x8_t*>(qp + 16 * c2);
+  }
+  const float sc = __builtin_fabsf(a.scale) * LOG2E;
+  const unsigned flip = a.scale < 0.f ? 0x80008000u : 0u;
+
+  // ---- tiles: 64 ring slots each (the pairs start at different ones), then 64 drafted keys
+  const int nring = (nvalid + TILE_KEYS - 1) / TILE_KEYS, ntile = nring + 1;
+  const int rot = (int)(pair % (unsigned)max(nring, 1));
+  auto ring_base = [&](int t) { const int s = t + rot; return (s < nring ? s : s - nring) * TILE_KEYS; };
+  constexpr int PK = TILE_KEYS * CH / 2;          // packed: 16-byte pieces of codes in a tile
+  constexpr int PT = PACKED ? (PK + 255) / 256 : 1;   // for the fewest threads (TREE_TILE_MIN_WAVES)
+  u32x4_t ck[PT], cv[PT];
+  uint8_t sk[PT], sv[PT];
+  // requests tile t for `buf`: rows behind the last one are read as that one (their weight is 0)
+  lds_byte* const lds = (lds_byte*)smem;
+  auto request = [&](int t, int buf) {
+    const bool nodes = t >= nring;
+    if (PACKED && !nodes) {
+      if constexpr (PACKED) {
+        const int base = ring_base(t);
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+          const int x = threadIdx.x + i * blockDim.x;
+          if (x < PK) {
+            const size_t r = (size_t)min(base + x / (CH / 2), nvalid - 1), c = x % (CH / 2);
+            ck[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint8_t*>(kr) + r * D + 16 * c);
+            cv[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint8_t*>(vr) + r * D + 16 * c);
+            sk[i] = krs[r * SB + c / 2];
+            sv[i] = vrs[r * SB + c / 2];
+          }
+        }
+      }
+    } else {
+      const uint16_t* ks_ = nodes ? kn : reinterpret_cast<const uint16_t*>(kr) + (size_t)ring_base(t) * D;
+      const uint16_t* vs_ = nodes ? vn : reinterpret_cast<const uint16_t*>(vr) + (size_t)ring_base(t) * D;
+      const size_t stride = nodes ? nstride : D;
+      const int have = nodes ? cnt : nvalid - ring_base(t);
+      for (int b = w; b < TG::NB; b += nwave) {
+        tile_block<D>(ks_, stride, have, lds + buf * 2 * KT, b, lane);
+        tile_block<D>(vs_, stride, have, lds + buf * 2 * KT + KT, b, lane);
+      }
+    }
+  };
+  // the requested tile is in `buf`, for this thread's part
+  auto deliver = [&](int t, int buf) {
+    if (PACKED && t < nring) {
+      if constexpr (PACKED) {
+        unsigned char *K = smem + buf * 2 * KT, *V = K + KT;
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+          const int x = threadIdx.x + i * blockDim.x;
+          if (x < PK) {
+            const int r = x / (CH / 2), c = x % (CH / 2);
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+              const u32x4_t codes = kv ? cv[i] : ck[i];
+              const float f = scale_of(kv ? sv[i] : sk[i]);
+              uint32_t t8[8];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) unpack_bf16x4(codes[j], f, t8[2 * j], t8[2 * j + 1]);
+              *reinterpret_cast<u32x4_t*>(tile_chunk<D>(kv ? V : K, r, 2 * c)) = u32x4_t{t8[0], t8[1], t8[2], t8[3]};
+              *reinterpret_cast<u32x4_t*>(tile_chunk<D>(kv ? V : K, r, 2 * c + 1)) = u32x4_t{t8[4], t8[5], t8[6], t8[7]};
+            }
+          }
+        }
+      }
+    } else wait_vmem();
+  };
+  if (sp < ntile) request(sp, 0);
+  const TreeNodes node = tree_nodes(up, W, lane);
+  const unsigned long long anc = shfl64(node.anc, node_of), left = shfl64(node.left, node_of);
+  const int depth = __popcll(anc) - 1;
+  int dmax = depth;
+#pragma unroll
+  for (int s = 1; s < 32; s <<= 1) dmax = max(dmax, __shfl_xor(dmax, s));
+  dmax = __builtin_amdgcn_readfirstlane(dmax);
+  int dall = lane < cnt ? node.depth() : 0;   // of the sequence's nodes: all waves agree on it
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) dall = max(dall, __shfl_xor(dall, s));
+  dall = __builtin_amdgcn_readfirstlane(dall);
+#pragma unroll
+  for (int c2 = 0; c2 < NC2; ++c2) q[c2] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, q[c2]) ^ flip);
+
+  // ---- softmax branch
+  const LaneOff<D> lo = make_lane_off<D>(lane);
+  f32x16_t acc[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[ct][i] = 0.f;
+  float m = -1.0e30f, l = 0.f;
+  int buf = 0;
+  if (sp < ntile) {
+    deliver(sp, 0);
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int t = sp; t < ntile; t += nsplit) {
+    if (t + nsplit < ntile) request(t + nsplit, buf ^ 1);
+    const lds_byte *K = lds + buf * 2 * KT, *V = K + KT;
+    const bool nodes = t >= nring;
+    const int base = nodes ? 0 : ring_base(t);
+    if (live) {
+      // both halves of the tile together: one maximum, and the products of either fill the other's waits
+      f32x16_t s[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[h][i] = 0.f;
+#pragma unroll
+      for (int c2 = 0; c2 < NC2; ++c2)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) s[h] = mfma32(tile_row<D>(K, lo, 32 * h, c2), q[c2], s[h]);
+      if (nodes) {
+        const unsigned long long see = (anc & ~left) >> (4 * hl);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[h][i] = (unsigned)(see >> (32 * h)) >> (8 * (i / 4) + i % 4) & 1 ? s[h][i] : -INFINITY;
+      } else {
+        const int youngest = base < slot0 && slot0 < base + TILE_KEYS ? 0 : age(base);
+        if (base + TILE_KEYS > nvalid || youngest <= dmax) {   // wave-uniform
+          const int s0 = opaque(base + 4 * hl);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int slot = s0 + 32 * h + 8 * (i / 4) + i % 4, j = slot < nvalid ? age(slot) : -1;
+              s[h][i] = j > depth ? s[h][i] : -INFINITY;
+            }
+        }
+      }
+      float mx = fmaxf(s[0][15], s[1][15]);
+#pragma unroll
+      for (int i = 0; i < 15; ++i) mx = max3(mx, s[0][i], s[1][i]);
+      mx = half_max(mx) * sc;
+      if (__any(mx > m + 8.f)) {   // (a running maximum stays while no score is far above it)
+        const float top = fmaxf(m, mx), alpha = fast_exp2(m - top);
+        m = top;
+        l *= alpha;
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) acc[ct] *= alpha;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float pr[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { pr[i] = fast_exp2(__builtin_fmaf(s[h][i], sc, -m)); l += pr[i]; }
+        // (one bf16 term, as in the layer's forward: the output's own rounding is as large)
+        const bf16x8_t pw[2] = {pack_bf16x8(pr), pack_bf16x8(pr + 8)};
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) acc[ct] = mfma32(tile_trp<D>(V, lo, 32 * h + 16 * kk, ct), pw[kk], acc[ct]);
+      }
+    }
+    if (t + nsplit < ntile) deliver(t + nsplit, buf ^ 1);
+    __syncthreads();
+    buf ^= 1;
+  }
+  l = half_sum(l);
+
+  // ---- linear branch.  phi(q) is formed a piece at a time
+  f32x16_t acr[NCT];
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acr[ct][i] = 0.f;
+  if (p + dall >= W) {
+#pragma unroll
+    for (int c2 = 0; c2 < NC2; ++c2) q[c2] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, q[c2]) ^ flip);
+    float fm = 0.f, fz = 1.f;
+    if (a.phi == PHI_SOFTMAX) {
+      float x[8], s = 0.f;
+      fm = -INFINITY;
+#pragma unroll
+      for (int c2 = 0; c2 < NC2; ++c2) {
+        unpack_bf16x8(q[c2], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) fm = fmaxf(fm, x[i]);
+      }
+      fm = half_max(fm);
+#pragma unroll
+      for (int c2 = 0; c2 < NC2; ++c2) {
+        unpack_bf16x8(q[c2], x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += fast_exp2((x[i] - fm) * LOG2E);
+      }
+      fz = 1.f / half_sum(s);
+    }
+    auto feature = [&](int c2, bf16x8_t& hi, bf16x8_t& lw) {
+      float x[8];
+      u32x4_t raw = __builtin_bit_cast(u32x4_t, q[c2]);   // (not what a loop would keep of all pieces in registers)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[i] = (unsigned)opaque((int)raw[i]);
+      unpack_bf16x8(__builtin_bit_cast(bf16x8_t, raw), x);
+      if (a.phi == PHI_SOFTMAX) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fast_exp2((x[i] - fm) * LOG2E) * fz;
+      } else if (a.phi == PHI_RELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = fmaxf(x[i], 0.f);
+      }
+      split2(x, hi, lw);
+    };
+    // keys that leave, 32 at a time: ring tokens by age 0 .. min(dall, W - 1), then (paths longer than the window) drafted ones
+    const int nage = min(dall + 1, W), sets = (nage + 31) / 32, all = sets + (dall >= W ? (cnt + 31) / 32 : 0);
+    unsigned char *Fh = smem, *Fl = smem + KT / 2, *Vt = smem + KT;
+#pragma unroll 1
+    for (int x = nsplit - 1 - sp; x < all; x += nsplit) {
+      // a thread has eight features of a row
+      for (int e = threadIdx.x; e < 32 * CH; e += blockDim.x) {
+        const int r = e / CH, c = e % CH, t = 32 * x + r;
+        u32x4_t kb = {0, 0, 0, 0}, vb = {0, 0, 0, 0};
+        if (x < sets) {
+          if (t < nage && t >= W - p) {
+            const size_t slot = slot0 + t < W ? slot0 + t : slot0 + t - W;
+            if constexpr (PACKED) {
+              const u32x2_t k8 = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(kr) + slot * D + 8 * c);
+              const u32x2_t v8 = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(vr) + slot * D + 8 * c);
+              const float fk = scale_of(krs[slot * SB + c / 4]), fv = scale_of(vrs[slot * SB + c / 4]);
+              uint32_t y[8];
+              unpack_bf16x4(k8[0], fk, y[0], y[1]);
+              unpack_bf16x4(k8[1], fk, y[2], y[3]);
+              unpack_bf16x4(v8[0], fv, y[4], y[5]);
+              unpack_bf16x4(v8[1], fv, y[6], y[7]);
+              kb = u32x4_t{y[0], y[1], y[2], y[3]};
+              vb = u32x4_t{y[4], y[5], y[6], y[7]};
+            } else {
+              kb = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint16_t*>(kr) + slot * D + 8 * c);
+              vb = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint16_t*>(vr) + slot * D + 8 * c);
+            }
+          }
+        } else if (t - 32 * sets < cnt) {
+          kb = *reinterpret_cast<const u32x4_t*>(kn + (size_t)(t - 32 * sets) * nstride + 8 * c);
+          vb = *reinterpret_cast<const u32x4_t*>(vn + (size_t)(t - 32 * sets) * nstride + 8 * c);
+        }
+        float f[8];
+        unpack_bf16x8(__builtin_bit_cast(bf16x8_t, kb), f);
+        if (a.phi == PHI_SOFTMAX) {
+          float mx = f[0], s = 0.f;
+#pragma unroll
+          for (int i = 1; i < 8; ++i) mx = fmaxf(mx, f[i]);
+          mx = lanes_max<CH>(mx);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) { f[i] = fast_exp2((f[i] - mx) * LOG2E); s += f[i]; }
+          s = 1.f / lanes_sum<CH>(s);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] *= s;
+        } else if (a.phi == PHI_RELU) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = fmaxf(f[i], 0.f);
+        }
+        bf16x8_t hi, lw;
+        split2(f, hi, lw);
+        *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Fh, r, c)) = hi;
+        *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Fl, r, c)) = lw;
+        *reinterpret_cast<u32x4_t*>(tile_chunk<D>(Vt, r, c)) = vb;
+      }
+      __syncthreads();
+      if (live) {
+        f32x16_t s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int c2 = 0; c2 < NC2; ++c2) {
+          bf16x8_t hi, lw;
+          feature(c2, hi, lw);
+          __builtin_amdgcn_sched_barrier(0);
+          const bf16x8_t kh = tile_row<D>(lds, lo, 0, c2), kl = tile_row<D>(lds + KT / 2, lo, 0, c2);
+          s = mfma32(kl, hi, s);
+          s = mfma32(kh, lw, s);
+          s = mfma32(kh, hi, s);
+        }
+        // which of the 32 keys this lane's row has left behind, from bit 4 hl on
+        auto below = [](int k) { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1; };
+        unsigned see = x < sets ? below(min(depth, W - 1) + 1 - 32 * x) & ~below(W - p - 32 * x) : (unsigned)(left >> (32 * (x - sets)));
+        see >>= 4 * hl;
+        float y[16], z[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = see >> (8 * (i / 4) + i % 4) & 1 ? s[i] : 0.f;
+        bf16x8_t ph[2] = {pack_bf16x8(y), pack_bf16x8(y + 8)}, pl[2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+          unpack_bf16x8(ph[kk], z + 8 * kk);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[8 * kk + i] = y[8 * kk + i] - z[8 * kk + i];
+          pl[kk] = pack_bf16x8(z + 8 * kk);
+        }
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+          for (int kk = 0; kk < 2; ++kk) {
+            const bf16x8_t v = tile_trp<D>(lds + KT, lo, 16 * kk, ct);
+            acr[ct] = mfma32(v, pl[kk], acr[ct]);
+            acr[ct] = mfma32(v, ph[kk], acr[ct]);
+          }
+      }
+      __syncthreads();
+    }
+    // the state as two terms [feature][value]; of SPLIT work-groups each takes some of the 16-feature pieces
+    if (p > W) {
+      unsigned char *Sh = smem, *Sl = smem + D * TG::ROWB;
+      const float* S = a.state + (size_t)pair * D * D;
+      for (int e = threadIdx.x; e < D * CH; e += blockDim.x) {
+        const int r = e / CH, c = e % CH;
+        if (SPLIT && (r / 16) % nsplit != sp) continue;
+        const f32x4_t u = *reinterpret_cast<const f32x4_t*>(S + (size_t)r * D + 8 * c), v = *reinterpret_cast<const f32x4_t*>(S + (size_t)r * D + 8 * c + 4);
+        float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
+        bf16x8_t hi, lw;
+        split2(x, hi, lw);
+        *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Sh, r, c)) = hi;
+        *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Sl, r, c)) = lw;
+      }
+      __syncthreads();
+      if (live) {
+        const LaneOffN<D> ln = make_lane_off_n<D>(lane);
+#pragma unroll
+        for (int c2 = 0; c2 < NC2; ++c2) {
+          if (SPLIT && c2 % nsplit != sp) continue;
+          bf16x8_t hi, lw;
+          feature(c2, hi, lw);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int ct = 0; ct < NCT; ++ct) {
+            const bf16x8_t sh = tile_trn<D>(lds, ln, 16 * c2, ct), sl = tile_trn<D>(lds + D * TG::ROWB, ln, 16 * c2, ct);
+            acr[ct] = mfma32(sl, hi, acr[ct]);
+            acr[ct] = mfma32(sh, lw, acr[ct]);
+            acr[ct] = mfma32(sh, hi, acr[ct]);
+          }
+        }
+      }
+    }
+  }
+  // ---- SPLIT: the sums of all work-groups of these rows, by the one that arrives last (see SplitArgs).  A lane has the features
+  // 32 ct + 8 b + 4 hl ..+3 of its row
+  const bool mine = row0 + 32 * w + r32 < nrows;
+  if constexpr (SPLIT) {
+    constexpr int LINE = SplitArgs::row(D);
+    const size_t cell = (size_t)pair * a.blocks + block;
+    const rsrc_t mem = make_rsrc(split.part + cell * split.n * rows_wg * LINE, (unsigned)(split.n * rows_wg * LINE * 4));
+    auto line = [&](int k) { return ((k * rows_wg + 32 * w + r32) * LINE + 4 * hl) * 4; };
+    auto four = [](const f32x16_t& x, int b) { return f32x4_t{x[4 * b], x[4 * b + 1], x[4 * b + 2], x[4 * b + 3]}; };
+    if (mine) {
+      const int at = line(sp);
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          put_shared16(mem, four(acc[ct], b), at + 4 * (32 * ct + 8 * b));
+          put_shared16(mem, four(acr[ct], b), at + 4 * (D + 32 * ct + 8 * b));
+        }
+      if (hl == 0) put_shared16(mem, f32x4_t{m, l, 0.f, 0.f}, at + 8 * D);
+    }
+    if (!arrive_last(split.ticket + cell, split.nonce, nsplit)) return;
+    m = -1.0e30f;
+    for (int k = 0; k < nsplit; ++k) m = fmaxf(m, get_shared16(mem, line(k) - 16 * hl + 8 * D)[0]);
+    l = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[ct][i] = acr[ct][i] = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < nsplit; ++k) {
+      const int at = line(k);
+      const f32x4_t ml = get_shared16(mem, at - 16 * hl + 8 * D);
+      const float f = fast_exp2(ml[0] - m);
+      l += f * ml[1];
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const f32x4_t x = get_shared16(mem, at + 4 * (32 * ct + 8 * b)), y = get_shared16(mem, at + 4 * (D + 32 * ct + 8 * b));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) { acc[ct][4 * b + i] += f * x[i]; acr[ct][4 * b + i] += y[i]; }
+        }
+    }
+  }
+  if (!live) return;
+  // ---- combination (Sec. 3.2)
+  const float inv = 1.f / l;
+  float s1 = 0.f, s2 = 0.f, z = inv * 0.f;
+#pragma unroll
+  for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      acc[ct][i] *= inv;
+      s1 += acc[ct][i] * acc[ct][i];
+      s2 += acr[ct][i] * acr[ct][i];
+      z += acc[ct][i] * 0.f + acr[ct][i] * 0.f;
+    }
+  s1 = half_sum(s1);
+  s2 = half_sum(s2);
+  z = half_sum(z);
+  const bool bad = mine && !(z == 0.f);
+  if (mine && !bad) {
+    const float r1 = rsqrtf(s1 / D + a.eps), r2 = rsqrtf(s2 / D + a.eps);
+    const int head = g * G + row % G;
+    bf16_t* o = a.o + (((size_t)n * M + node_of) * a.Hq + head) * D + 4 * hl;
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct) { acc[ct] *= r1; acr[ct] *= r2; }
+    auto gains = [&](const float* gain, f32x16_t (&x)[NCT]) {
+      const float* gp = gain + head * D + 4 * hl;
+#pragma unroll
+      for (int ct = 0; ct < NCT; ++ct) {
+        f32x4_t y[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) __builtin_memcpy(&y[b], gp + 32 * ct + 8 * b, 16);   // (aligned like a float)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[ct][i] *= y[i / 4][i % 4];
+      }
+    };
+    if (a.gs) gains(a.gs, acc);
+    if (a.gr) gains(a.gr, acr);
+#pragma unroll
+    for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        store4(o + 32 * ct + 8 * b, f32x4_t{acc[ct][4 * b] + acr[ct][4 * b], acc[ct][4 * b + 1] + acr[ct][4 * b + 1],
+                                            acc[ct][4 * b + 2] + acr[ct][4 * b + 2], acc[ct][4 * b + 3] + acr[ct][4 * b + 3]});
+  }
+  unsigned long long again = __ballot(bad && hl == 0);
+  while (again) {
+    const int from = __builtin_ctzll(again);
+    again &= again - 1;
+    const int r = __shfl(row, from), i = r / G;
+    tree_row_again<bf16_t, RT, D>(a, n, g, r, shfl64(node.anc, i), shfl64(node.left, i), lane);
+  }
+}
+
+template <typename RT, int D, bool SPLIT>
+void launch_tree_tile(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
+  const size_t bytes = tree_tile_lds<D>();
+  static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void*>(tree_tile_kernel<RT, D, SPLIT>),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+  (void)attr;
+  const TreeArgs<bf16_t, RT> a = tree_args<bf16_t, RT>(td, t, pl);
+  std::conditional_t<SPLIT, SplitArgs, NoSplit> split;
+  if constexpr (SPLIT)
+    split = {(float*)((char*)td.workspace + pl.part_off), (unsigned long long*)td.workspace, td.nonce, pl.nsplit, 0};
+  const long long grid = ((long long)td.N * td.Hkv + 7) / 8 * 8 * pl.blocks * (SPLIT ? pl.nsplit : 1);
+  tree_tile_kernel<RT, D, SPLIT><<<(unsigned)grid, pl.NW * 64, bytes, st>>>(a, split);
+}
+template <typename RT, int D>
+void pick_tree_tile(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
+  if (td.workspace && pl.nsplit > 1) launch_tree_tile<RT, D, true>(td, t, pl, st);
+  else launch_tree_tile<RT, D, false>(td, t, pl, st);
+}
+
+}  // namespace
+
+}  // namespace rattn
