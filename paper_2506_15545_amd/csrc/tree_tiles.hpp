@@ -15,7 +15,10 @@ namespace {
 
 constexpr int TILE_KEYS = 64;
 static_assert(TREE_TILE_MIN_WAVES == 4, "packed pieces of a tile that a thread has on the way");
-template <int D> constexpr size_t tree_tile_lds() { return 4 * (size_t)TileGeom<D>::KT; }   // two buffers of a K and a V tile
+// two buffers of a K and a V tile, and the gains of up to TILE_GAINS query heads of a KV head (more are read from memory): fetched
+// with the rest of the inputs, where the end of a work-group waited for them (13 k of 196 k cycles)
+constexpr int TILE_GAINS = 8;
+template <int D> constexpr size_t tree_tile_lds() { return 4 * (size_t)TileGeom<D>::KT + 2 * TILE_GAINS * D * 4; }
 
 // 16 bytes of a tile: chunk c (8 features) of row r
 template <int D> __device__ __forceinline__ unsigned char* tile_chunk(unsigned char* tile, int r, int c) {
@@ -170,6 +173,13 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
       }
     } else wait_vmem();
   };
+  float* glds = reinterpret_cast<float*>(smem + 4 * KT);   // [2][G][D]
+  const bool staged = G <= TILE_GAINS;
+  if (staged)
+    for (int e = threadIdx.x; e < G * D; e += blockDim.x) {
+      if (a.gs) glds[e] = a.gs[g * G * D + e];
+      if (a.gr) glds[G * D + e] = a.gr[g * G * D + e];
+    }
   if (sp < ntile) request(sp, 0);
   const TreeNodes node = tree_nodes(up, W, lane);
   const unsigned long long anc = shfl64(node.anc, node_of), left = shfl64(node.left, node_of);
@@ -503,19 +513,20 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
     bf16_t* o = a.o + (((size_t)n * M + node_of) * a.Hq + head) * D + 4 * hl;
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) { acc[ct] *= r1; acr[ct] *= r2; }
-    auto gains = [&](const float* gain, f32x16_t (&x)[NCT]) {
-      const float* gp = gain + head * D + 4 * hl;
+    auto gains = [&](const float* gp, f32x16_t (&x)[NCT]) {
 #pragma unroll
-      for (int ct = 0; ct < NCT; ++ct) {
-        f32x4_t y[4];
+      for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) __builtin_memcpy(&y[b], gp + 32 * ct + 8 * b, 16);   // (aligned like a float)
+        for (int b = 0; b < 4; ++b) {
+          f32x4_t y;
+          __builtin_memcpy(&y, gp + 32 * ct + 8 * b, 16);   // (aligned like a float)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[ct][i] *= y[i / 4][i % 4];
-      }
+          for (int i = 0; i < 4; ++i) x[ct][4 * b + i] *= y[i];
+        }
     };
-    if (a.gs) gains(a.gs, acc);
-    if (a.gr) gains(a.gr, acr);
+    const int hd = (row % G) * D + 4 * hl;
+    if (a.gs) { if (staged) gains(glds + hd, acc); else gains(a.gs + g * G * D + hd, acc); }
+    if (a.gr) { if (staged) gains(glds + G * D + hd, acr); else gains(a.gr + g * G * D + hd, acr); }
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
