@@ -256,7 +256,7 @@ struct TreePlan {
   int CT, KG, NW, blocks, nsplit, KW, tiles;
   size_t part_off, bytes;   // workspace: tickets from offset 0 (nothing: 0 bytes)
 };
-constexpr int TREE_TILE_MIN_WAVES = 4;   // of a work-group with `tiles`
+constexpr int TREE_TILE_WAVES = 4;   // of a work-group with `tiles`
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed);
 void tree_step(const TreeDims& td, int dtype, const TreeTensors& t, hipStream_t st);
 void tree_commit(const TreeDims& td, int dtype, const TreeTensors& t, const int32_t* accepted, hipStream_t st);

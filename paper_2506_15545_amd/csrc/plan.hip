@@ -120,13 +120,18 @@ DecodeSplit decode_split(const DecodeDims& dd, int esize) {
   //   128 pairs, W = 512 16.1 | 16.8 | 17.4;  W = 2048 38.1 | 34.1 | 34.2 | 39.4 (not taken: rings with 100 - 400 tokens
   //   10.7 | 11.6);  192, W = 2048 35.5 | 39.2 | 39.6
   //   32 pairs, D = 64, W = 512 7.8 | 9.9;  4 pairs, fp32, W = 512 18.5 | 15.4 | 12.6 | 11.2 | 11.8
+  // Packed rings (work to unpack for each byte): 32 KB each, four or more, up to 256 of them, or 512 of 128 KB.  One | as split, bf16,
+  // D = 128: 4 pairs, W = 512 12.2 | 9.8;  1024 15.5 | 10.5;  2048 22.3 | 11.8;  4096 35.3 | 13.1;  32, 512 13.2 | 11.1;  2048 24.1 |
+  // 15.0;  64, 512 13.4 | 12.2;  2048 24.7 | 16.2;  128, 2048 26.0 | 22.7.  Two are as slow as one (12.2 | 11.8, 24.1 | 24.2); not
+  // taken: 128 pairs, W = 512 14.5 | 15.0;  192, 2048 32.9 | 34.8.  D = 64, 64 pairs, W = 2048 14.5 | 11.7;  512 8.2 | 9.0 (not taken)
   DecodeSplit s = {1, dd.W, 0, 0};
   const long long pairs = (long long)dd.N * dd.Hkv, ring = 2ll * dd.W * dd.D * esize;
-  if (dd.G > 16 || ring < 256 << 10) return s;
-  const int share = 64 << 10;
+  const bool packed = esize == 1;
+  const int share = packed ? 32 << 10 : 64 << 10, least = packed ? 4 : 2, most = packed ? ring >= 512 << 10 && pairs > 64 ? 512 : 256 : 128;
+  if (dd.G > 16 || ring < 4 * share) return s;
   s.n = DEC_MAX_SPLIT;
-  while (s.n > 1 && (ring / s.n < share || pairs * s.n > 128)) s.n /= 2;
-  if (s.n < 2) return s;
+  while (s.n > 1 && (ring / s.n < share || pairs * s.n > most)) s.n /= 2;
+  if (s.n < least) { s.n = 1; return s; }
   s.rows = (int)(share * (long long)dd.W / ring);
   s.part_off = ((size_t)pairs * 8 + 255) / 256 * 256;
   s.bytes = s.part_off + (size_t)pairs * s.n * dd.G * (2 * dd.D + 4) * 4;
@@ -148,27 +153,21 @@ ExportPlan export_plan(const LayerDims& dm) {
 
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   TreePlan p = {1, 8, 8, 1, 1, 6, 0, 0, 0};
-  const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32;
+  const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32, sets = (td.W + keys - 1) / keys + (td.M + keys - 1) / keys, pieces = td.D / keys + 1;
   const long long pairs = (long long)td.N * td.Hkv;
-  auto workspace = [&](int per) {
-    const long long groups = pairs * p.blocks;
-    if (p.nsplit > 1) {
-      p.part_off = ((size_t)groups * 8 + 255) / 256 * 256;
-      p.bytes = p.part_off + (size_t)groups * p.nsplit * per * (2 * td.D + 4) * 4;
-    }
-    return p;
-  };
-  if (dtype == 1 && rows > 64) {
-    const int t32 = (rows + 31) / 32;
+  // Keys through LDS where waves that fetch them themselves would be more than the chip holds at once (work-groups of 64 rows, one
+  // per CU).  us, direct | tiles, bf16, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.9 | 34.8, 57.8 | 68.2; of 256 46.2 | 37.3,
+  // 107 | 72; 128 of 128 rows 26.3 | 35.1, 59.2 | 69.3; 192 of 96 42.6 | 34.9, 107 | 72; 64 of 256 26.3 | 36.1, 53.5 | 69.3; of 512
+  // 44.1 | 38.5, 102 | 71.  D = 64: 64 of 256 16.4 | 22.4, 36.3 | 48.0; of 512 28.9 | 23.7, 66.6 | 49.3
+  // (packed: 64 of 256 rows, W = 2048 66 | 49).  Packed rings of D = 128, which they unpack on the way (at the cost of registers), from
+  // twice as many on: 192 of 128 42.1 | 47.6, 104 | 123; 320 of 128 62 | 64, 153 | 143; 128 of 512 82 | 61, 201 | 141
+  if (dtype == 1 && rows > 64 && pairs * ((rows + 63) / 64) > (packed && td.D == 128 ? 512 : 256)) {
     p.tiles = 1;
     p.CT = 2;
     p.KG = 1;
-    p.blocks = (t32 + 3) / 4;
-    p.NW = 4;
-    const int tiles = (td.W + 63) / 64 + 1;
-    p.nsplit = DEC_MAX_SPLIT;
-    while (p.nsplit > 1 && (pairs * p.blocks * p.nsplit > 256 || tiles < 2 * p.nsplit)) p.nsplit /= 2;
-    return workspace(32 * p.NW);
+    p.NW = TREE_TILE_WAVES;
+    p.blocks = ((rows + 31) / 32 + p.NW - 1) / p.NW;
+    return p;
   }
   if (dtype == 0) {
     p.KG = rows <= 16 ? 8 : 4;
@@ -176,20 +175,36 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
     p.CT = 2;
     p.KG = rows <= 32 ? 8 : 4;
   }
+  // Four waves where there is too little for eight: bf16, D = 128, eight | four, 4 pairs of 16 rows, W = 64 10.2 | 10.2, 256 12.2 | 10.8,
+  // 512 12.9 | 12.8; of 32 rows 13.3 | 13.5, 15.9 | 14.1, 16.3 | 16.4; 256 pairs of 16 rows 12.6 | 12.5, 16.9 | 14.3, 19.2 | 18.9;
+  // packed, of 32 rows 15.8 | 15.7, 17.0 | 15.8, 17.9 | 19.3
   const int group = 16 * p.CT;
-  if (rows <= group && pairs >= 256) p.KG = p.NW = 4;
+  if (dtype == 1 && rows <= group && sets > 4 && sets <= 12) p.KG = p.NW = 4;
   const int per = p.NW / p.KG * group;
   p.blocks = (rows + per - 1) / per;
   const long long groups = pairs * p.blocks;
-  const int sets = (td.W + keys - 1) / keys + (td.M + keys - 1) / keys, pieces = td.D / keys + 1;
-  // waves by what either branch has to do: a piece of the state counts one and a half sets of keys
-  int kl = (int)((p.KG * 3ll * pieces + (2 * sets + 3 * pieces) / 2) / (2 * sets + 3 * pieces));
+  // waves by what either branch has to do: a piece of the state counts two sets of keys (bf16, D = 128, W = 512, 1 | 2 | 3 | 4 of eight
+  // waves for it: 8 pairs of 16 rows 15.0 | 14.0 | 13.1 | 13.3, 128 of 24 20.9 | 20.1 | 18.7 | 19.2; W = 2048, 8 of 24 16.9 | 16.8 |
+  // 16.9 | 19.2)
+  int kl = (p.KG * 4 * pieces + sets + 2 * pieces) / (2 * (sets + 2 * pieces));
   if (kl < 1) kl = 1;
   if (kl > p.KG / 2) kl = p.KG / 2;
   p.KW = p.KG - kl;
-  p.nsplit = DEC_MAX_SPLIT;
-  while (p.nsplit > 1 && (groups * p.nsplit > 256 || sets < p.KW * p.nsplit)) p.nsplit /= 2;
-  return workspace(per);
+  // Work-groups that share a pair's keys, up to 256 in all, by how many sets of keys each wave has: joining them costs 2 to 4 us,
+  // for two as much as for four.  1 | 2 | 4 | 8, D = 128, bf16:
+  //   4 pairs of 16 rows, W = 512 12.9 | 12.9 | 13.1 | 12.9;  1024 16.2 | 14.8 | 13.6 | 14.1;  2048 25.1 | 18.0 | 15.4 | 14.4;  4096
+  //   44.8 | 27.7 | 18.8 | 15.6;  of 64 rows, W = 256 17.1 | 18.9 | 17.6 | 19.1;  512 20.3 | 20.9 | 18.9 | 20.3;  4096 86 | 51 | 33 | 25
+  //   64 pairs of 32 rows, W = 512 17.5 | 18.3 | 18.3 | 28.5;  1024 20.4 | 21.1 | 19.4 | 31.0;  4096 60 | 43 | 37 | 43
+  //   128 pairs of 32 rows, W = 1024 21.4 | 23.2 | 30.5;  2048 38.2 | 35.8 | 41.6;  of 64, 512 24.5 | 26.4 | 35.4;  1024 33.2 | 28.5 | 41.1
+  //   fp32, 4 pairs of 16 rows, W = 512 24.3 | 18.6 | 14.7 | 15.8;  2048 57.6 | 35.6 | 24.1 | 18.7;  128, 512 26.4 | 22.2 | 28.6
+  p.nsplit = sets >= 18 * p.KW ? 8 : sets >= 5 * p.KW ? 4 : 1;
+  if (groups * p.nsplit > 256 && p.nsplit == 8) p.nsplit = 4;
+  if (groups * p.nsplit > 256) p.nsplit = groups * 2 <= 256 && sets >= 6 * p.KW ? 2 : 1;
+  if (p.nsplit > 1) {
+    p.part_off = ((size_t)groups * 8 + 255) / 256 * 256;
+    p.bytes = p.part_off + (size_t)groups * p.nsplit * per * (2 * td.D + 4) * 4;
+  }
+  return p;
 }
 
 }  // namespace rattn

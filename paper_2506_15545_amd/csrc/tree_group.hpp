@@ -1020,14 +1020,20 @@ template <typename IO, typename RT, int D>
 void pick_tree(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
 #define RATTN_TREE(CT_, KG_, NW_)                                                                   \
   if (pl.CT == CT_ && pl.KG == KG_ && pl.NW == NW_) {                                               \
-    if (td.workspace && pl.nsplit > 1) launch_tree<IO, RT, D, CT_, KG_, NW_, true>(td, t, pl, st);  \
-    else launch_tree<IO, RT, D, CT_, KG_, NW_, false>(td, t, pl, st);                               \
+    if constexpr (NW_ == 8) {                                                                       \
+      if (td.workspace && pl.nsplit > 1) {                                                          \
+        launch_tree<IO, RT, D, CT_, KG_, NW_, true>(td, t, pl, st);                                 \
+        return;                                                                                     \
+      }                                                                                             \
+    }                                                                                               \
+    launch_tree<IO, RT, D, CT_, KG_, NW_, false>(td, t, pl, st);                                    \
     return;                                                                                         \
   }
   RATTN_TREE(1, 8, 8)
-  RATTN_TREE(1, 4, 4)
-  RATTN_TREE(1, 4, 8)
-  if constexpr (sizeof(IO) == 2) {
+  if constexpr (sizeof(IO) == 4) {
+    RATTN_TREE(1, 4, 8)
+  } else {
+    RATTN_TREE(1, 4, 4)
     RATTN_TREE(2, 8, 8)
     RATTN_TREE(2, 4, 4)
     RATTN_TREE(2, 4, 8)

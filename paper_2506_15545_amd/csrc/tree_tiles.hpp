@@ -14,7 +14,7 @@ namespace rattn {
 namespace {
 
 constexpr int TILE_KEYS = 64;
-static_assert(TREE_TILE_MIN_WAVES == 4, "packed pieces of a tile that a thread has on the way");
+constexpr int TILE_WAVES = TREE_TILE_WAVES, TILE_THREADS = 64 * TILE_WAVES;
 // two buffers of a K and a V tile, and the gains of up to TILE_GAINS query heads of a KV head (more are read from memory): fetched
 // with the rest of the inputs, where the end of a work-group waited for them (13 k of 196 k cycles)
 constexpr int TILE_GAINS = 8;
@@ -27,11 +27,22 @@ template <int D> __device__ __forceinline__ unsigned char* tile_chunk(unsigned c
 // lds_row, lds_trp and lds_trn (mfma.hpp) of tiles whose address is known to lie in LDS: which of two buffers it is changes from
 // tile to tile, and through a general pointer the compiler would ask where it points
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
-// 1024 bytes of a tile (block b: rows RPB b ..) straight from memory; rows from nrows on are read as row nrows - 1
-template <int D> __device__ __forceinline__ void tile_block(const uint16_t* rows, size_t stride, int nrows, lds_byte* tile, int b, int lane) {
+// A wave's share of a tile (blocks blk0 .. blk0 + NBLK - 1 of 1024 bytes) straight from memory: whole tiles of rows that lie one
+// behind the other (which `dl` is for) from a scalar base; of others the rows from nrows on are read as row nrows - 1
+template <int D, int NBLK>
+__device__ __forceinline__ void tile_fetch(const uint16_t* rows, size_t stride, int nrows, lds_byte* tile, int blk0, const DmaLane<D>& dl, int lane) {
   typedef TileGeom<D> G;
-  const int r = b * G::RPB + lane / G::CH, c = (lane % G::CH) ^ swz<D>(r);
-  dma16(rows + (size_t)min(r, nrows - 1) * stride + c * 8, (unsigned)(size_t)(tile + b * 1024));
+  if (nrows >= 64 && stride == D) {
+#pragma unroll
+    for (int i = 0; i < NBLK; ++i)
+      dma16s(rows + (size_t)(blk0 + i) * G::RPB * stride, dl.off[i % G::NV], (unsigned)(size_t)(tile + (blk0 + i) * 1024));
+  } else {
+#pragma unroll
+    for (int i = 0; i < NBLK; ++i) {
+      const int r = (blk0 + i) * G::RPB + lane / G::CH, c = (lane % G::CH) ^ swz<D>(r);
+      dma16(rows + (size_t)min(r, nrows - 1) * stride + c * 8, (unsigned)(size_t)(tile + (blk0 + i) * 1024));
+    }
+  }
 }
 template <int D> __device__ __forceinline__ bf16x8_t tile_row(const lds_byte* tile, const LaneOff<D>& lo, int R0, int c2) {
   return *reinterpret_cast<const __attribute__((address_space(3))) bf16x8_t*>(tile + lo.row[c2] + R0 * TileGeom<D>::ROWB);
@@ -69,32 +80,29 @@ __device__ __forceinline__ void split2(float (&x)[8], bf16x8_t& hi, bf16x8_t& lo
   lo = pack_bf16x8(t);
 }
 
-template <typename RT, int D, bool SPLIT>
-__global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> a, std::conditional_t<SPLIT, SplitArgs, NoSplit> split) {
+// SOFT: the softmax map.  (Left to run time, the choice cut every piece of phi out of the products around it.)
+template <typename RT, int D, bool SOFT>
+__global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> a) {
   constexpr bool PACKED = sizeof(RT) == 1;
   typedef TileGeom<D> TG;
   constexpr int KT = TG::KT, CH = TG::CH, SB = scale_bytes(D), NCT = D / 32, NC2 = D / 16;
   extern __shared__ __align__(16) unsigned char smem[];   // [2][K, V][64 rows]
-  const int lane = lane_id(), w = wave_id(), nwave = blockDim.x >> 6, r32 = lane & 31, hl = lane >> 5;
-  const int W = a.W, G = a.G, M = a.M, Hkv = a.Hkv, rows_wg = 32 * nwave;
-  const unsigned pairs = a.N * Hkv, per = (pairs + 7) / 8 * 8 * a.blocks;   // (as in tree_kernel)
-  const int sp = SPLIT ? blockIdx.x / per : 0;
-  const unsigned id = SPLIT ? blockIdx.x % per : blockIdx.x;
-  const unsigned pair = id / (8 * a.blocks) * 8 + id % 8;
-  const int block = id / 8 % a.blocks;
+  const int lane = lane_id(), w = wave_id(), r32 = lane & 31, hl = lane >> 5;
+  const int W = a.W, G = a.G, M = a.M, Hkv = a.Hkv, rows_wg = 32 * TILE_WAVES;
+  const unsigned pairs = a.N * Hkv, pair = blockIdx.x / (8 * a.blocks) * 8 + blockIdx.x % 8;   // (as in tree_kernel)
+  const int block = blockIdx.x / 8 % a.blocks;
   if (pair >= pairs) return;
   const int g = pair % Hkv, n = pair / Hkv;
   const int p = a.pos[n], cnt = a.count ? min(a.count[n], M) : M;
   const int row0 = block * rows_wg, nrows = cnt * G;
   if (row0 >= nrows || p < 0) return;
-  const int nsplit = SPLIT ? split.n : 1;
   const int slot0 = p % W, nvalid = min(p, W);
   const RT *kr = a.k_ring + (size_t)pair * W * D, *vr = a.v_ring + (size_t)pair * W * D;
   const uint8_t* krs = PACKED ? a.ks + (size_t)pair * W * SB : nullptr;
   const uint8_t* vrs = PACKED ? a.vs + (size_t)pair * W * SB : nullptr;
   const bf16_t *kn = a.k + ((size_t)n * M * Hkv + g) * D, *vn = a.v + ((size_t)n * M * Hkv + g) * D;
   const size_t nstride = (size_t)Hkv * D;
-  auto age = [&](int slot) { return slot - slot0 + (slot < slot0 ? W : 0); };
+  auto age = [&](int slot) { const int j = slot - slot0; return j + (j >> 31 & W); };
 
   // ---- this wave's rows: lane r32 has row r32's operand, features 16 c2 + 8 hl ..+7.  A negative scale goes to q's signs, so
   // that the largest score is that of the largest product
@@ -115,72 +123,84 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
   const int rot = (int)(pair % (unsigned)max(nring, 1));
   auto ring_base = [&](int t) { const int s = t + rot; return (s < nring ? s : s - nring) * TILE_KEYS; };
   constexpr int PK = TILE_KEYS * CH / 2;          // packed: 16-byte pieces of codes in a tile
-  constexpr int PT = PACKED ? (PK + 255) / 256 : 1;   // for the fewest threads (TREE_TILE_MIN_WAVES)
-  u32x4_t ck[PT], cv[PT];
-  uint8_t sk[PT], sv[PT];
-  // requests tile t for `buf`: rows behind the last one are read as that one (their weight is 0)
+  constexpr int PT = PACKED ? (PK + TILE_THREADS - 1) / TILE_THREADS : 1;
+  u32x4_t codes[PT];
+  uint8_t code_scale[PT];
+  // requests tile t for `buf`: rows behind the last one are read as that one (their weight is 0).  The codes of a packed ring pass
+  // through registers, the keys' while the tile before has its first products and the values' while it has its second ones
   lds_byte* const lds = (lds_byte*)smem;
+  const DmaLane<D> dma_lane = make_dma_lane<D>(lane, D);
+  auto request_codes = [&](int t, const RT* ring, const uint8_t* scales) {
+    if constexpr (PACKED) {
+      const int base = ring_base(t);
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const int x = threadIdx.x + i * TILE_THREADS;
+        if (x < PK) {
+          const size_t r = (size_t)min(base + x / (CH / 2), nvalid - 1), c = x % (CH / 2);
+          codes[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint8_t*>(ring) + r * D + 16 * c);
+          code_scale[i] = scales[r * SB + c / 2];
+        }
+      }
+    }
+  };
+  auto deliver_codes = [&](unsigned char* tile) {
+    if constexpr (PACKED) {
+#pragma unroll
+      for (int i = 0; i < PT; ++i) {
+        const int x = threadIdx.x + i * TILE_THREADS;
+        if (x < PK) {
+          const int r = x / (CH / 2), c = x % (CH / 2);
+          const float f = scale_of(code_scale[i]);
+          uint32_t t8[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) unpack_bf16x4(codes[i][j], f, t8[2 * j], t8[2 * j + 1]);
+          *reinterpret_cast<u32x4_t*>(tile_chunk<D>(tile, r, 2 * c)) = u32x4_t{t8[0], t8[1], t8[2], t8[3]};
+          *reinterpret_cast<u32x4_t*>(tile_chunk<D>(tile, r, 2 * c + 1)) = u32x4_t{t8[4], t8[5], t8[6], t8[7]};
+        }
+      }
+    }
+  };
   auto request = [&](int t, int buf) {
     const bool nodes = t >= nring;
     if (PACKED && !nodes) {
-      if constexpr (PACKED) {
-        const int base = ring_base(t);
-#pragma unroll
-        for (int i = 0; i < PT; ++i) {
-          const int x = threadIdx.x + i * blockDim.x;
-          if (x < PK) {
-            const size_t r = (size_t)min(base + x / (CH / 2), nvalid - 1), c = x % (CH / 2);
-            ck[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint8_t*>(kr) + r * D + 16 * c);
-            cv[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint8_t*>(vr) + r * D + 16 * c);
-            sk[i] = krs[r * SB + c / 2];
-            sv[i] = vrs[r * SB + c / 2];
-          }
-        }
-      }
+      request_codes(t, kr, krs);
     } else {
       const uint16_t* ks_ = nodes ? kn : reinterpret_cast<const uint16_t*>(kr) + (size_t)ring_base(t) * D;
       const uint16_t* vs_ = nodes ? vn : reinterpret_cast<const uint16_t*>(vr) + (size_t)ring_base(t) * D;
       const size_t stride = nodes ? nstride : D;
       const int have = nodes ? cnt : nvalid - ring_base(t);
-      for (int b = w; b < TG::NB; b += nwave) {
-        tile_block<D>(ks_, stride, have, lds + buf * 2 * KT, b, lane);
-        tile_block<D>(vs_, stride, have, lds + buf * 2 * KT + KT, b, lane);
-      }
+      constexpr int NBLK = TG::NB / TILE_WAVES;
+      static_assert(NBLK % TG::NV == 0, "a wave's blocks start where the swizzle does");
+      tile_fetch<D, NBLK>(ks_, stride, have, lds + buf * 2 * KT, NBLK * w, dma_lane, lane);
+      tile_fetch<D, NBLK>(vs_, stride, have, lds + buf * 2 * KT + KT, NBLK * w, dma_lane, lane);
     }
   };
-  // the requested tile is in `buf`, for this thread's part
-  auto deliver = [&](int t, int buf) {
+  // half way: packed keys are in `buf`, the values requested.  At the end: the tile is in `buf`, for this thread's part
+  auto half_way = [&](int t, int buf) {
     if (PACKED && t < nring) {
-      if constexpr (PACKED) {
-        unsigned char *K = smem + buf * 2 * KT, *V = K + KT;
-#pragma unroll
-        for (int i = 0; i < PT; ++i) {
-          const int x = threadIdx.x + i * blockDim.x;
-          if (x < PK) {
-            const int r = x / (CH / 2), c = x % (CH / 2);
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-              const u32x4_t codes = kv ? cv[i] : ck[i];
-              const float f = scale_of(kv ? sv[i] : sk[i]);
-              uint32_t t8[8];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) unpack_bf16x4(codes[j], f, t8[2 * j], t8[2 * j + 1]);
-              *reinterpret_cast<u32x4_t*>(tile_chunk<D>(kv ? V : K, r, 2 * c)) = u32x4_t{t8[0], t8[1], t8[2], t8[3]};
-              *reinterpret_cast<u32x4_t*>(tile_chunk<D>(kv ? V : K, r, 2 * c + 1)) = u32x4_t{t8[4], t8[5], t8[6], t8[7]};
-            }
-          }
-        }
-      }
-    } else wait_vmem();
+      deliver_codes(smem + buf * 2 * KT);
+      request_codes(t, vr, vrs);
+    }
+  };
+  auto deliver = [&](int t, int buf) {
+    if (PACKED && t < nring) deliver_codes(smem + buf * 2 * KT + KT);
+    else wait_vmem();
   };
   float* glds = reinterpret_cast<float*>(smem + 4 * KT);   // [2][G][D]
   const bool staged = G <= TILE_GAINS;
-  if (staged)
-    for (int e = threadIdx.x; e < G * D; e += blockDim.x) {
-      if (a.gs) glds[e] = a.gs[g * G * D + e];
-      if (a.gr) glds[G * D + e] = a.gr[g * G * D + e];
+  constexpr int NG = TILE_GAINS * D / TILE_THREADS;
+  float gain[2][NG];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int e = threadIdx.x + i * TILE_THREADS;
+    gain[0][i] = gain[1][i] = 0.f;
+    if (staged && e < G * D) {
+      if (a.gs) gain[0][i] = a.gs[g * G * D + e];
+      if (a.gr) gain[1][i] = a.gr[g * G * D + e];
     }
-  if (sp < ntile) request(sp, 0);
+  }
+  request(0, 0);
   const TreeNodes node = tree_nodes(up, W, lane);
   const unsigned long long anc = shfl64(node.anc, node_of), left = shfl64(node.left, node_of);
   const int depth = __popcll(anc) - 1;
@@ -192,6 +212,26 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) dall = max(dall, __shfl_xor(dall, s));
   dall = __builtin_amdgcn_readfirstlane(dall);
+  // maximum and sum of phi(q), while the first tile is on its way
+  float fm = 0.f, fz = 1.f;
+  if (SOFT && p + dall >= W) {
+    float x[8], s = 0.f;
+    fm = -INFINITY;
+#pragma unroll
+    for (int c2 = 0; c2 < NC2; ++c2) {
+      unpack_bf16x8(q[c2], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) fm = fmaxf(fm, x[i]);
+    }
+    fm = half_max(fm);
+#pragma unroll
+    for (int c2 = 0; c2 < NC2; ++c2) {
+      unpack_bf16x8(q[c2], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += fast_exp2((x[i] - fm) * LOG2E);
+    }
+    fz = 1.f / half_sum(s);
+  }
 #pragma unroll
   for (int c2 = 0; c2 < NC2; ++c2) q[c2] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, q[c2]) ^ flip);
 
@@ -202,15 +242,19 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
   for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[ct][i] = 0.f;
-  float m = -1.0e30f, l = 0.f;
+  float m = -1.0e30f, l = 0.f, lsum[4] = {0.f, 0.f, 0.f, 0.f};
   int buf = 0;
-  if (sp < ntile) {
-    deliver(sp, 0);
-    __syncthreads();
+  half_way(0, 0);
+  deliver(0, 0);
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const int e = threadIdx.x + i * TILE_THREADS;
+    if (staged && e < G * D) { glds[e] = gain[0][i]; glds[G * D + e] = gain[1][i]; }
   }
+  __syncthreads();
 #pragma unroll 1
-  for (int t = sp; t < ntile; t += nsplit) {
-    if (t + nsplit < ntile) request(t + nsplit, buf ^ 1);
+  for (int t = 0; t < ntile; ++t) {
+    if (t + 1 < ntile) request(t + 1, buf ^ 1);
     const lds_byte *K = lds + buf * 2 * KT, *V = K + KT;
     const bool nodes = t >= nring;
     const int base = nodes ? 0 : ring_base(t);
@@ -225,6 +269,14 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
       for (int c2 = 0; c2 < NC2; ++c2)
 #pragma unroll
         for (int h = 0; h < 2; ++h) s[h] = mfma32(tile_row<D>(K, lo, 32 * h, c2), q[c2], s[h]);
+      // operand reads four products ahead (left to itself the compiler waits for every read right in front of its product)
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * NC2; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      if constexpr (PACKED) { if (t + 1 < ntile) half_way(t + 1, buf ^ 1); }
       if (nodes) {
         const unsigned long long see = (anc & ~left) >> (4 * hl);
 #pragma unroll
@@ -239,8 +291,8 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int slot = s0 + 32 * h + 8 * (i / 4) + i % 4, j = slot < nvalid ? age(slot) : -1;
-              s[h][i] = j > depth ? s[h][i] : -INFINITY;
+              const int slot = s0 + 32 * h + 8 * (i / 4) + i % 4;
+              s[h][i] = (slot < nvalid) & (age(slot) > depth) ? s[h][i] : -INFINITY;
             }
         }
       }
@@ -251,28 +303,46 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
       if (__any(mx > m + 8.f)) {   // (a running maximum stays while no score is far above it)
         const float top = fmaxf(m, mx), alpha = fast_exp2(m - top);
         m = top;
-        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lsum[i] *= alpha;
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) acc[ct] *= alpha;
       }
+      // The second products in explicit order: a half's operands are read while the half before is worked on, the second half's
+      // exponentials stand between the first one's products (left to the compiler: 8 % more at W = 2048).  (One bf16 term for the
+      // probabilities, as in the layer's forward: the output's own rounding is as large.)
+      constexpr int NP = 2 * NCT;
+      bf16x8_t v[NP], pw[2];
+      float pr[16];
+      auto operand = [&](int h, int i) { return tile_trp<D>(V, lo, 32 * h + 16 * (i / NCT), i % NCT); };
+      auto prob = [&](int h, int i) { pr[i] = fast_exp2(__builtin_fmaf(s[h][i], sc, -m)); lsum[i & 3] += pr[i]; };
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float pr[16];
+      for (int i = 0; i < NP; ++i) v[i] = operand(0, i);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { pr[i] = fast_exp2(__builtin_fmaf(s[h][i], sc, -m)); l += pr[i]; }
-        // (one bf16 term, as in the layer's forward: the output's own rounding is as large)
-        const bf16x8_t pw[2] = {pack_bf16x8(pr), pack_bf16x8(pr + 8)};
+      for (int i = 0; i < 16; ++i) prob(0, i);
+      pw[0] = pack_bf16x8(pr);
+      pw[1] = pack_bf16x8(pr + 8);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct)
+      for (int i = 0; i < NP; ++i) {
+        acc[i % NCT] = mfma32(v[i], pw[i / NCT], acc[i % NCT]);
 #pragma unroll
-          for (int kk = 0; kk < 2; ++kk) acc[ct] = mfma32(tile_trp<D>(V, lo, 32 * h + 16 * kk, ct), pw[kk], acc[ct]);
+        for (int j = 16 / NP * i; j < 16 / NP * (i + 1); ++j) prob(1, j);
+        v[i] = operand(1, i);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      pw[0] = pack_bf16x8(pr);
+      pw[1] = pack_bf16x8(pr + 8);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) acc[i % NCT] = mfma32(v[i], pw[i / NCT], acc[i % NCT]);
     }
-    if (t + nsplit < ntile) deliver(t + nsplit, buf ^ 1);
+    if (PACKED && !live && t + 1 < ntile) half_way(t + 1, buf ^ 1);
+    if (t + 1 < ntile) deliver(t + 1, buf ^ 1);
     __syncthreads();
     buf ^= 1;
   }
-  l = half_sum(l);
+  l = half_sum((lsum[0] + lsum[1]) + (lsum[2] + lsum[3]));
 
   // ---- linear branch.  phi(q) is formed a piece at a time
   f32x16_t acr[NCT];
@@ -283,37 +353,19 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
   if (p + dall >= W) {
 #pragma unroll
     for (int c2 = 0; c2 < NC2; ++c2) q[c2] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, q[c2]) ^ flip);
-    float fm = 0.f, fz = 1.f;
-    if (a.phi == PHI_SOFTMAX) {
-      float x[8], s = 0.f;
-      fm = -INFINITY;
-#pragma unroll
-      for (int c2 = 0; c2 < NC2; ++c2) {
-        unpack_bf16x8(q[c2], x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) fm = fmaxf(fm, x[i]);
-      }
-      fm = half_max(fm);
-#pragma unroll
-      for (int c2 = 0; c2 < NC2; ++c2) {
-        unpack_bf16x8(q[c2], x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += fast_exp2((x[i] - fm) * LOG2E);
-      }
-      fz = 1.f / half_sum(s);
-    }
+    const float least = a.phi == PHI_RELU ? 0.f : -INFINITY;   // of the other two maps' values
     auto feature = [&](int c2, bf16x8_t& hi, bf16x8_t& lw) {
       float x[8];
       u32x4_t raw = __builtin_bit_cast(u32x4_t, q[c2]);   // (not what a loop would keep of all pieces in registers)
 #pragma unroll
       for (int i = 0; i < 4; ++i) raw[i] = (unsigned)opaque((int)raw[i]);
       unpack_bf16x8(__builtin_bit_cast(bf16x8_t, raw), x);
-      if (a.phi == PHI_SOFTMAX) {
+      if constexpr (SOFT) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = fast_exp2((x[i] - fm) * LOG2E) * fz;
-      } else if (a.phi == PHI_RELU) {
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = fmaxf(x[i], 0.f);
+        for (int i = 0; i < 8; ++i) x[i] = fmaxf(x[i], least);
       }
       split2(x, hi, lw);
     };
@@ -321,9 +373,9 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
     const int nage = min(dall + 1, W), sets = (nage + 31) / 32, all = sets + (dall >= W ? (cnt + 31) / 32 : 0);
     unsigned char *Fh = smem, *Fl = smem + KT / 2, *Vt = smem + KT;
 #pragma unroll 1
-    for (int x = nsplit - 1 - sp; x < all; x += nsplit) {
+    for (int x = 0; x < all; ++x) {
       // a thread has eight features of a row
-      for (int e = threadIdx.x; e < 32 * CH; e += blockDim.x) {
+      for (int e = threadIdx.x; e < 32 * CH; e += TILE_THREADS) {
         const int r = e / CH, c = e % CH, t = 32 * x + r;
         u32x4_t kb = {0, 0, 0, 0}, vb = {0, 0, 0, 0};
         if (x < sets) {
@@ -351,7 +403,7 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
         }
         float f[8];
         unpack_bf16x8(__builtin_bit_cast(bf16x8_t, kb), f);
-        if (a.phi == PHI_SOFTMAX) {
+        if constexpr (SOFT) {
           float mx = f[0], s = 0.f;
 #pragma unroll
           for (int i = 1; i < 8; ++i) mx = fmaxf(mx, f[i]);
@@ -361,9 +413,9 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
           s = 1.f / lanes_sum<CH>(s);
 #pragma unroll
           for (int i = 0; i < 8; ++i) f[i] *= s;
-        } else if (a.phi == PHI_RELU) {
+        } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] = fmaxf(f[i], 0.f);
+          for (int i = 0; i < 8; ++i) f[i] = fmaxf(f[i], least);
         }
         bf16x8_t hi, lw;
         split2(f, hi, lw);
@@ -376,15 +428,19 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
         f32x16_t s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        bf16x8_t hi, lw, kh = tile_row<D>(lds, lo, 0, 0), kl = tile_row<D>(lds + KT / 2, lo, 0, 0);
+        feature(0, hi, lw);
 #pragma unroll
-        for (int c2 = 0; c2 < NC2; ++c2) {
-          bf16x8_t hi, lw;
-          feature(c2, hi, lw);
-          __builtin_amdgcn_sched_barrier(0);
-          const bf16x8_t kh = tile_row<D>(lds, lo, 0, c2), kl = tile_row<D>(lds + KT / 2, lo, 0, c2);
+        for (int c2 = 0; c2 < NC2; ++c2) {   // the next piece of phi(q), and of phi(k), behind this one's products
           s = mfma32(kl, hi, s);
           s = mfma32(kh, lw, s);
           s = mfma32(kh, hi, s);
+          if (c2 + 1 < NC2) {
+            kh = tile_row<D>(lds, lo, 0, c2 + 1);
+            kl = tile_row<D>(lds + KT / 2, lo, 0, c2 + 1);
+            feature(c2 + 1, hi, lw);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
         // which of the 32 keys this lane's row has left behind, from bit 4 hl on
         auto below = [](int k) { return k <= 0 ? 0u : k >= 32 ? ~0u : (1u << k) - 1; };
@@ -412,84 +468,53 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
       }
       __syncthreads();
     }
-    // the state as two terms [feature][value]; of SPLIT work-groups each takes some of the 16-feature pieces
+    // the state as two terms [feature][value]
     if (p > W) {
       unsigned char *Sh = smem, *Sl = smem + D * TG::ROWB;
       const float* S = a.state + (size_t)pair * D * D;
-      for (int e = threadIdx.x; e < D * CH; e += blockDim.x) {
-        const int r = e / CH, c = e % CH;
-        if (SPLIT && (r / 16) % nsplit != sp) continue;
-        const f32x4_t u = *reinterpret_cast<const f32x4_t*>(S + (size_t)r * D + 8 * c), v = *reinterpret_cast<const f32x4_t*>(S + (size_t)r * D + 8 * c + 4);
-        float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
-        bf16x8_t hi, lw;
-        split2(x, hi, lw);
-        *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Sh, r, c)) = hi;
-        *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Sl, r, c)) = lw;
+      constexpr int NE = D * CH / TILE_THREADS, BATCH = NE < 4 ? NE : 4;
+#pragma unroll 1
+      for (int e0 = threadIdx.x; e0 < D * CH; e0 += BATCH * TILE_THREADS) {
+        f32x4_t u[BATCH][2];   // (the batch is requested before any of it is worked on)
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) u[b][k] = *reinterpret_cast<const f32x4_t*>(S + (size_t)(e0 + b * TILE_THREADS) * 8 + 4 * k);
+#pragma unroll
+        for (int b = 0; b < BATCH; ++b) {
+          const int e = e0 + b * TILE_THREADS, r = e / CH, c = e % CH;
+          float x[8] = {u[b][0][0], u[b][0][1], u[b][0][2], u[b][0][3], u[b][1][0], u[b][1][1], u[b][1][2], u[b][1][3]};
+          bf16x8_t hi, lw;
+          split2(x, hi, lw);
+          *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Sh, r, c)) = hi;
+          *reinterpret_cast<bf16x8_t*>(tile_chunk<D>(Sl, r, c)) = lw;
+        }
       }
       __syncthreads();
       if (live) {
         const LaneOffN<D> ln = make_lane_off_n<D>(lane);
+        bf16x8_t hi, lw;
+        feature(0, hi, lw);
 #pragma unroll
-        for (int c2 = 0; c2 < NC2; ++c2) {
-          if (SPLIT && c2 % nsplit != sp) continue;
-          bf16x8_t hi, lw;
-          feature(c2, hi, lw);
-          __builtin_amdgcn_sched_barrier(0);
+        for (int c2 = 0; c2 < NC2; ++c2) {   // operands, the next piece of phi(q), products
+          bf16x8_t sh[NCT], sl[NCT];
 #pragma unroll
           for (int ct = 0; ct < NCT; ++ct) {
-            const bf16x8_t sh = tile_trn<D>(lds, ln, 16 * c2, ct), sl = tile_trn<D>(lds + D * TG::ROWB, ln, 16 * c2, ct);
-            acr[ct] = mfma32(sl, hi, acr[ct]);
-            acr[ct] = mfma32(sh, lw, acr[ct]);
-            acr[ct] = mfma32(sh, hi, acr[ct]);
+            sh[ct] = tile_trn<D>(lds, ln, 16 * c2, ct);
+            sl[ct] = tile_trn<D>(lds + D * TG::ROWB, ln, 16 * c2, ct);
           }
+          const bf16x8_t h0 = hi, l0 = lw;
+          if (c2 + 1 < NC2) feature(c2 + 1, hi, lw);
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) acr[ct] = mfma32(k == 0 ? sl[ct] : sh[ct], k == 1 ? l0 : h0, acr[ct]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     }
   }
-  // ---- SPLIT: the sums of all work-groups of these rows, by the one that arrives last (see SplitArgs).  A lane has the features
-  // 32 ct + 8 b + 4 hl ..+3 of its row
   const bool mine = row0 + 32 * w + r32 < nrows;
-  if constexpr (SPLIT) {
-    constexpr int LINE = SplitArgs::row(D);
-    const size_t cell = (size_t)pair * a.blocks + block;
-    const rsrc_t mem = make_rsrc(split.part + cell * split.n * rows_wg * LINE, (unsigned)(split.n * rows_wg * LINE * 4));
-    auto line = [&](int k) { return ((k * rows_wg + 32 * w + r32) * LINE + 4 * hl) * 4; };
-    auto four = [](const f32x16_t& x, int b) { return f32x4_t{x[4 * b], x[4 * b + 1], x[4 * b + 2], x[4 * b + 3]}; };
-    if (mine) {
-      const int at = line(sp);
-#pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          put_shared16(mem, four(acc[ct], b), at + 4 * (32 * ct + 8 * b));
-          put_shared16(mem, four(acr[ct], b), at + 4 * (D + 32 * ct + 8 * b));
-        }
-      if (hl == 0) put_shared16(mem, f32x4_t{m, l, 0.f, 0.f}, at + 8 * D);
-    }
-    if (!arrive_last(split.ticket + cell, split.nonce, nsplit)) return;
-    m = -1.0e30f;
-    for (int k = 0; k < nsplit; ++k) m = fmaxf(m, get_shared16(mem, line(k) - 16 * hl + 8 * D)[0]);
-    l = 0.f;
-#pragma unroll
-    for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[ct][i] = acr[ct][i] = 0.f;
-#pragma unroll 1
-    for (int k = 0; k < nsplit; ++k) {
-      const int at = line(k);
-      const f32x4_t ml = get_shared16(mem, at - 16 * hl + 8 * D);
-      const float f = fast_exp2(ml[0] - m);
-      l += f * ml[1];
-#pragma unroll
-      for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const f32x4_t x = get_shared16(mem, at + 4 * (32 * ct + 8 * b)), y = get_shared16(mem, at + 4 * (D + 32 * ct + 8 * b));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) { acc[ct][4 * b + i] += f * x[i]; acr[ct][4 * b + i] += y[i]; }
-        }
-    }
-  }
   if (!live) return;
   // ---- combination (Sec. 3.2)
   const float inv = 1.f / l;
@@ -543,22 +568,18 @@ __global__ __launch_bounds__(512, 2) void tree_tile_kernel(TreeArgs<bf16_t, RT> 
   }
 }
 
-template <typename RT, int D, bool SPLIT>
+template <typename RT, int D, bool SOFT>
 void launch_tree_tile(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
   const size_t bytes = tree_tile_lds<D>();
-  static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void*>(tree_tile_kernel<RT, D, SPLIT>),
+  static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void*>(tree_tile_kernel<RT, D, SOFT>),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
   (void)attr;
-  const TreeArgs<bf16_t, RT> a = tree_args<bf16_t, RT>(td, t, pl);
-  std::conditional_t<SPLIT, SplitArgs, NoSplit> split;
-  if constexpr (SPLIT)
-    split = {(float*)((char*)td.workspace + pl.part_off), (unsigned long long*)td.workspace, td.nonce, pl.nsplit, 0};
-  const long long grid = ((long long)td.N * td.Hkv + 7) / 8 * 8 * pl.blocks * (SPLIT ? pl.nsplit : 1);
-  tree_tile_kernel<RT, D, SPLIT><<<(unsigned)grid, pl.NW * 64, bytes, st>>>(a, split);
+  const long long grid = ((long long)td.N * td.Hkv + 7) / 8 * 8 * pl.blocks;
+  tree_tile_kernel<RT, D, SOFT><<<(unsigned)grid, TILE_THREADS, bytes, st>>>(tree_args<bf16_t, RT>(td, t, pl));
 }
 template <typename RT, int D>
 void pick_tree_tile(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
-  if (td.workspace && pl.nsplit > 1) launch_tree_tile<RT, D, true>(td, t, pl, st);
+  if (td.phi == PHI_SOFTMAX) launch_tree_tile<RT, D, true>(td, t, pl, st);
   else launch_tree_tile<RT, D, false>(td, t, pl, st);
 }
 
