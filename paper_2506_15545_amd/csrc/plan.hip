@@ -178,8 +178,11 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   // Four waves where there is too little for eight: bf16, D = 128, eight | four, 4 pairs of 16 rows, W = 64 10.2 | 10.2, 256 12.2 | 10.8,
   // 512 12.9 | 12.8; of 32 rows 13.3 | 13.5, 15.9 | 14.1, 16.3 | 16.4; 256 pairs of 16 rows 12.6 | 12.5, 16.9 | 14.3, 19.2 | 18.9;
   // packed, of 32 rows 15.8 | 15.7, 17.0 | 15.8, 17.9 | 19.3
+  // More pairs than CUs (two such work-groups on one), of 24 rows, W = 64, 512, 1024: 288 25.1 | 17.6, 33.2 | 27.9, 50.9 | 48.5; 512 26.8 |
+  // 18.8, 41.7 | 37.9, 64.0 | 68.6; 768, W = 1024 93.5 | 105; packed, 512 26.9 | 19.0, 33.4 | 27.9, 48.6 | 47.2; D = 64 16.9 | 12.5,
+  // 22.2 | 18.2, 34.3 | 33.1
   const int group = 16 * p.CT;
-  if (dtype == 1 && rows <= group && sets > 4 && sets <= 12) p.KG = p.NW = 4;
+  if (dtype == 1 && rows <= group && (pairs > 256 ? sets <= 24 : sets > 4 && sets <= 12)) p.KG = p.NW = 4;
   const int per = p.NW / p.KG * group;
   p.blocks = (rows + per - 1) / per;
   const long long groups = pairs * p.blocks;
