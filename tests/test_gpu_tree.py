@@ -69,7 +69,10 @@ SHAPES = [  # N, M, Hq, Hkv, W, pos, spread
     (2, 64, 1, 1, 64, [63, 64], 1), (2, 64, 1, 1, 63, [64, 500], 1), (1, 64, 6, 1, 100, [99], 9),
     (2, 17, 20, 1, 130, [5, 1000], 4), (3, 13, 5, 1, 65, [64, 65, 66], 2),   # rows that no tile of 16 divides
     (9, 3, 8, 8, 96, [40 * i for i in range(9)], 2),     # 72 pairs: no multiple of the XCDs
-    (1, 6, 4, 1, 2049, [5000], 2), (2, 40, 8, 2, 700, [300, 9999], 6)]       # several work-groups for a ring
+    (1, 6, 4, 1, 2049, [5000], 2), (2, 40, 8, 2, 700, [300, 9999], 6),       # several work-groups for a ring
+    (1, 5, 2, 1, 4321, [9000], 1), (2, 8, 4, 1, 4096, [4095, 4097], 2), (1, 30, 4, 2, 4100, [70000], 3),
+    (3, 4, 4, 1, 200, [0, 199, 999], 2), (2, 8, 8, 2, 300, [299, 5000], 2),  # four waves: short windows, many pairs
+    (70, 3, 16, 4, 64, [7 * i for i in range(70)], 1), (65, 7, 16, 4, 333, [31 * i for i in range(65)], 3)]
 
 
 @pytest.mark.parametrize("packed", [False, True])
