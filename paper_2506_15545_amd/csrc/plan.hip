@@ -169,11 +169,23 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
     p.blocks = ((rows + 31) / 32 + p.NW - 1) / p.NW;
     return p;
   }
+  // Rows of a work-group: 16, so that there are many work-groups for the few; 32 or 64 (which read the ring less often) where those of
+  // 16 or 32 would be more than the CUs, or with long rings, which work-groups share, half as many.
+  // us, bf16, D = 128, W = 64, 512, 2048:        64 (32)           32                16
+  //   4 pairs of 48 rows                  15.2  18.3  21.7  13.1  15.9  19.5  10.4  12.8  15.8
+  //   32 of 128                           17.0  23.6  28.0  14.5  17.3  24.9  11.5  14.4  28.2
+  //   64 of 48                            16.3  21.2  26.2  14.0  17.1  24.9  11.6  14.1  28.5
+  //   64 of 128                           17.4  22.6  38.7  14.9  17.8  31.7  20.4  25.2  51.3
+  //   128 of 128                          18.7  25.7  59.5  27.4  33.0  65.2
+  //   128 of 24                                             13.8  17.5  34.7  11.4  15.3  36.2
+  //   fp32, 64 of 48 (32 | 16 rows)                         17.1  27.4  73.7  14.8  26.2  62.7
+  //   128 of 48                                             18.0  40.1   132  25.9  48.0   122
+  const long long by16 = pairs * ((rows + 15) / 16), by32 = pairs * ((rows + 31) / 32);
   if (dtype == 0) {
-    p.KG = rows <= 16 ? 8 : 4;
-  } else if (rows > 16) {
+    p.KG = rows <= 16 || by16 <= 256 ? 8 : 4;
+  } else if (rows > 16 && by16 * (sets >= 40 ? 2 : 1) > 256) {
     p.CT = 2;
-    p.KG = rows <= 32 ? 8 : 4;
+    p.KG = rows <= 32 || by32 <= 256 ? 8 : 4;
   }
   // Four waves where there is too little for eight: bf16, D = 128, eight | four, 4 pairs of 16 rows, W = 64 10.2 | 10.2, 256 12.2 | 10.8,
   // 512 12.9 | 12.8; of 32 rows 13.3 | 13.5, 15.9 | 14.1, 16.3 | 16.4; 256 pairs of 16 rows 12.6 | 12.5, 16.9 | 14.3, 19.2 | 18.9;
@@ -182,7 +194,7 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   // 18.8, 41.7 | 37.9, 64.0 | 68.6; 768, W = 1024 93.5 | 105; packed, 512 26.9 | 19.0, 33.4 | 27.9, 48.6 | 47.2; D = 64 16.9 | 12.5,
   // 22.2 | 18.2, 34.3 | 33.1
   const int group = 16 * p.CT;
-  if (dtype == 1 && rows <= group && (pairs > 256 ? sets <= 24 : sets > 4 && sets <= 12)) p.KG = p.NW = 4;
+  if (dtype == 1 && p.KG == 8 && (pairs > 256 ? sets <= 24 : sets > 4 && sets <= 12)) p.KG = p.NW = 4;
   const int per = p.NW / p.KG * group;
   p.blocks = (rows + per - 1) / per;
   const long long groups = pairs * p.blocks;

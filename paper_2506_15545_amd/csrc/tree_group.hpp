@@ -441,6 +441,19 @@ template <typename IO, typename RT> struct TreeArgs {
 
 constexpr size_t tree_lds_bytes(int D, int CT, int NW) { return (size_t)NW * 16 * CT * ((D + 4) + 2) * 4; }
 
+// Which (sequence, KV head) pair and which of its `blocks` work-group `id` has: eight pairs at a time, the blocks of each eight apart, so
+// that those that read the same ring sit on one XCD, at the same time; fewer than eight pairs are spread over all XCDs (4 pairs of 256
+// rows, W = 2048, 256 work-groups: 25.5 us on four XCDs, 16.4)
+__device__ __forceinline__ unsigned tree_pair(unsigned id, unsigned pairs, unsigned blocks, int& block) {
+  const unsigned side = pairs < 8 ? pairs : 8;
+  block = id / side % blocks;
+  return id / (side * blocks) * side + id % side;
+}
+inline long long tree_grid(const TreeDims& td, const TreePlan& pl) {
+  const long long pairs = (long long)td.N * td.Hkv, side = pairs < 8 ? pairs : 8;
+  return (pairs + side - 1) / side * side * pl.blocks;
+}
+
 // A row whose sums hold something that is no finite number, by a whole wave, key by key: only the keys that the row sees are
 // touched.  (The tiles multiply the others by 0, which is not 0 for an infinite or NaN feature.)
 template <typename IO, typename RT, int D>
@@ -580,12 +593,10 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
   float* ml = part + NW * 16 * CT * LD;       // [NW][16 CT][2]
   const int lane = lane_id(), w = wave_id(), r16 = lane & 15, q4 = lane >> 4;
   const int W = a.W, G = a.G, M = a.M, Hkv = a.Hkv;
-  // Eight pairs at a time, the blocks of each eight apart: those that read the same ring sit on one XCD, at the same time
-  const unsigned pairs = a.N * Hkv, per = (pairs + 7) / 8 * 8 * a.blocks;
+  const unsigned pairs = a.N * Hkv, per = SPLIT ? gridDim.x / split.n : gridDim.x;
   const int sp = SPLIT ? blockIdx.x / per : 0;
-  const unsigned id = SPLIT ? blockIdx.x % per : blockIdx.x;
-  const unsigned pair = id / (8 * a.blocks) * 8 + id % 8;
-  const int block = id / 8 % a.blocks;
+  int block;
+  const unsigned pair = tree_pair(SPLIT ? blockIdx.x % per : blockIdx.x, pairs, a.blocks, block);
   if (pair >= pairs) return;
   const int g = pair % Hkv, n = pair / Hkv;
   const int p = a.pos[n], cnt = a.count ? min(a.count[n], M) : M;
@@ -1012,7 +1023,7 @@ void launch_tree(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, h
   std::conditional_t<SPLIT, SplitArgs, NoSplit> split;
   if constexpr (SPLIT)
     split = {(float*)((char*)td.workspace + pl.part_off), (unsigned long long*)td.workspace, td.nonce, pl.nsplit, 0};
-  const long long grid = ((long long)td.N * td.Hkv + 7) / 8 * 8 * pl.blocks * (SPLIT ? pl.nsplit : 1);
+  const long long grid = tree_grid(td, pl) * (SPLIT ? pl.nsplit : 1);
   tree_kernel<IO, RT, D, CT, KG, NW, SPLIT><<<(unsigned)grid, NW * 64, bytes, st>>>(a, pl.KW, split);
 }
 

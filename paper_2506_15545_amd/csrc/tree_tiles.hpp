@@ -89,8 +89,8 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
   extern __shared__ __align__(16) unsigned char smem[];   // [2][K, V][64 rows]
   const int lane = lane_id(), w = wave_id(), r32 = lane & 31, hl = lane >> 5;
   const int W = a.W, G = a.G, M = a.M, Hkv = a.Hkv, rows_wg = 32 * TILE_WAVES;
-  const unsigned pairs = a.N * Hkv, pair = blockIdx.x / (8 * a.blocks) * 8 + blockIdx.x % 8;   // (as in tree_kernel)
-  const int block = blockIdx.x / 8 % a.blocks;
+  int block;
+  const unsigned pairs = a.N * Hkv, pair = tree_pair(blockIdx.x, pairs, a.blocks, block);
   if (pair >= pairs) return;
   const int g = pair % Hkv, n = pair / Hkv;
   const int p = a.pos[n], cnt = a.count ? min(a.count[n], M) : M;
@@ -574,8 +574,7 @@ void launch_tree_tile(const TreeDims& td, const TreeTensors& t, const TreePlan& 
   static const bool attr = hipFuncSetAttribute(reinterpret_cast<const void*>(tree_tile_kernel<RT, D, SOFT>),
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
   (void)attr;
-  const long long grid = ((long long)td.N * td.Hkv + 7) / 8 * 8 * pl.blocks;
-  tree_tile_kernel<RT, D, SOFT><<<(unsigned)grid, TILE_THREADS, bytes, st>>>(tree_args<bf16_t, RT>(td, t, pl));
+  tree_tile_kernel<RT, D, SOFT><<<(unsigned)tree_grid(td, pl), TILE_THREADS, bytes, st>>>(tree_args<bf16_t, RT>(td, t, pl));
 }
 template <typename RT, int D>
 void pick_tree_tile(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
