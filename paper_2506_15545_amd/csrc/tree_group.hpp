@@ -14,6 +14,9 @@
 // state is a "V" of D rows, whose "probabilities" are phi(q).
 // A wave has CT tiles of 16 rows and a share of the keys (of the ring sets, then of the sets of drafted keys); the KG waves that
 // share the rows meet in LDS, where 16 lanes take a row.  Several work-groups with the same keys lie side by side on one XCD.
+// Few sequences are bound by the way of one work-group through its inputs (12 nodes behind one sequence, 16 query and 4 KV heads, D = 128,
+// W = 512: 12 us, of which 3 are the launch and the walk of the tree, 3 the meeting and the rows' end), many by memory and by
+// what a CU takes in (64 sequences of 6 nodes, 32 query and 8 KV heads, packed rings of 512 slots: 25.6 us, 4.2 TB/s).
 #pragma once
 #include "packed.hpp"
 #include "ring_set.hpp"
@@ -476,7 +479,7 @@ __device__ void tree_row_again(const TreeArgs<IO, RT>& a, int n, int g, int row,
       bool in;
       if (t < W) {
         in = t > depth;
-        const int slot = slot0 + t < W ? slot0 + t : slot0 + t - W;
+        const int slot = t < W - slot0 ? slot0 + t : t - (W - slot0);
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
           k[e] = ring_value(kr, krs, (size_t)slot * D + lane + 64 * e);
@@ -799,7 +802,7 @@ __global__ __launch_bounds__(NW * 64, 2) void tree_kernel(TreeArgs<IO, RT> a, in
     depths(node);
     // Keys that leave: ring tokens in slots slot0 .., then 0 ..; then drafted ones, where a path is longer than the window.  Of the
     // waves the last come first (the first ones may have a piece of the state more)
-    const bool any = p + dmax >= W;
+    const bool any = p >= W - dmax;
     const int nleave = any ? min(dmax + 1, W) : 0, len0 = min(nleave, W - slot0), sets0 = (len0 + KEYS - 1) / KEYS;
     const int sets = sets0 + (nleave - len0 + KEYS - 1) / KEYS, nodes = any && dmax >= W ? (cnt + KEYS - 1) / KEYS : 0;
     auto leave_base = [&](int x) { return x < sets0 ? slot0 + x * KEYS : (x - sets0) * KEYS; };

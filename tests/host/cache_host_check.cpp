@@ -21,7 +21,8 @@ int main() {
   const int32_t* ix = (const int32_t*)x;
   float* fx = (float*)x;
   const int shapes[][5] = {{1, 1, 1, 64, 1},       {1, 16, 4, 128, 512},   {128, 32, 8, 128, 512}, {65535, 1, 1, 128, 9},
-                           {1, 65535, 65535, 64, 3}, {1, 4, 1, 128, 1 << 30}, {7, 320, 1, 64, 1000}, {3, 65535, 1, 128, 70000}};
+                           {1, 65535, 65535, 64, 3}, {1, 4, 1, 128, 1 << 30}, {7, 320, 1, 64, 1000}, {3, 65535, 1, 128, 70000},
+                           {1, 4, 1, 64, 0x7fffffff}, {24, 40, 8, 128, 2048}, {400, 8, 2, 64, 300}};
   for (auto& s : shapes)
     for (int dtype = 0; dtype < 2; ++dtype)
       for (int nodes : {1, 2, 3, 16, 17, 33, 63, 64})

@@ -173,6 +173,21 @@ def test_counts_and_sequences_without_work(dtype):
     assert all(torch.equal(keep[n][4], x[n][4]) for n in keep) and not torch.equal(keep["kr"][0], x["kr"][0])
 
 
+@pytest.mark.parametrize("N,M", [(1, 9), (140, 33)])
+def test_the_last_positions_of_an_int32(N, M):
+    """Positions whose tree passes 2^31 - 1: only whether the window is full and where it starts matter."""
+    W = 24
+    far = [2 ** 31 - 1 - i % 3 for i in range(N)]
+    x = make(N, M, 4, 2, 64, W, "bf16", [p % W + 40 * W for p in far], False, 8250, 1)
+    accepted = torch.full((N,), M - 1, dtype=torch.int32, device="cuda")
+    y = {n: (t.clone() if t is not None else None) for n, t in x.items()}
+    y["pos"] = torch.tensor(far, dtype=torch.int32, device="cuda")
+    assert torch.equal(step(x, 0.125), step(y, 0.125))
+    for z in (x, y):
+        rb.rattn_tree_commit(z["k"], z["v"], z["parent"], accepted, z["pos"], z["kr"], z["vr"], z["state"])
+    assert all(torch.equal(x[n], y[n]) for n in ("kr", "vr", "state"))
+
+
 def test_parents_that_are_no_earlier_node_are_the_last_token():
     W = 40
     x = make(1, 6, 4, 1, 64, W, "f32", [77], False, 7500, 2)
