@@ -6,7 +6,7 @@
 // layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
 // second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
 // phi(k) of the keys that leave, then the state, both as two bf16 terms.
-// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 96 us, 380 TFLOP/s; fetching their
+// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 91 us, 397 TFLOP/s; fetching their
 // own keys the waves take 164.  Bound by the operands from LDS (a wave reads all of a tile for its 32 rows: 2.1 of 4.2 k
 // cycles that the eight waves of a CU take for a tile each) and by the products and exponentials around them (2.0 and 1.6 k).
 #pragma once
@@ -21,6 +21,10 @@ constexpr int TILE_WAVES = TREE_TILE_WAVES, TILE_THREADS = 64 * TILE_WAVES;
 // two buffers of a K and a V tile, and the gains of up to TILE_GAINS query heads of a KV head (more are read from memory): fetched
 // with the rest of the inputs, where the end of a work-group waited for them (13 k of 196 k cycles)
 constexpr int TILE_GAINS = 8;
+// More work-groups than run at once (two on each of 256 CUs) take the sequences with the longest rings first: one that starts when
+// others end is a short one.  (24 sequences of 100 to 4000 tokens, 8 KV heads, 305 rows, W = 2048: 96 us in order,
+// 91 so; then the longest work-groups are what the rest waits for.)
+constexpr unsigned TILE_AT_ONCE = 512;
 template <int D> constexpr size_t tree_tile_lds() { return 4 * (size_t)TileGeom<D>::KT + 2 * TILE_GAINS * D * 4; }
 
 // 16 bytes of a tile: chunk c (8 features) of row r
@@ -93,9 +97,21 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
   const int lane = lane_id(), w = wave_id(), r32 = lane & 31, hl = lane >> 5;
   const int W = a.W, G = a.G, M = a.M, Hkv = a.Hkv, rows_wg = 32 * TILE_WAVES;
   int block;
-  const unsigned pairs = a.N * Hkv, pair = tree_pair(blockIdx.x, pairs, a.blocks, block);
+  const unsigned pairs = a.N * Hkv;
+  unsigned pair = tree_pair(blockIdx.x, pairs, a.blocks, block);
   if (pair >= pairs) return;
-  const int g = pair % Hkv, n = pair / Hkv;
+  const int g = pair % Hkv;
+  int n = pair / Hkv;
+  if (a.N <= 64 && gridDim.x > TILE_AT_ONCE) {
+    const int held = lane < a.N ? min(a.pos[lane], W) : -1;
+    int before = 0;
+    for (int i = 0; i < a.N; ++i) {
+      const int other = __builtin_amdgcn_readlane(held, i);
+      before += other > held || (other == held && i < lane);
+    }
+    n = (int)__builtin_ctzll(__ballot(lane < a.N && before == n));
+    pair = (unsigned)n * Hkv + g;
+  }
   const int p = a.pos[n], cnt = a.count ? min(a.count[n], M) : M;
   const int row0 = block * rows_wg, nrows = cnt * G;
   if (row0 >= nrows || p < 0) return;
