@@ -213,7 +213,7 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   //   64 pairs of 32 rows, W = 512 17.5 | 18.3 | 18.3 | 28.5;  1024 20.4 | 21.1 | 19.4 | 31.0;  4096 60 | 43 | 37 | 43
   //   128 pairs of 32 rows, W = 1024 21.4 | 23.2 | 30.5;  2048 38.2 | 35.8 | 41.6;  of 64, 512 24.5 | 26.4 | 35.4;  1024 33.2 | 28.5 | 41.1
   //   fp32, 4 pairs of 16 rows, W = 512 24.3 | 18.6 | 14.7 | 15.8;  2048 57.6 | 35.6 | 24.1 | 18.7;  128, 512 26.4 | 22.2 | 28.6
-  p.nsplit = sets >= 18 * p.KW ? 8 : sets >= 5 * p.KW ? 4 : 1;
+  p.nsplit = p.NW == 4 ? 1 : sets >= 18 * p.KW ? 8 : sets >= 5 * p.KW ? 4 : 1;
   if (groups * p.nsplit > 256 && p.nsplit == 8) p.nsplit = 4;
   if (groups * p.nsplit > 256) p.nsplit = groups * 2 <= 256 && sets >= 6 * p.KW ? 2 : 1;
   if (p.nsplit > 1) {

@@ -1034,7 +1034,7 @@ template <typename IO, typename RT, int D>
 void pick_tree(const TreeDims& td, const TreeTensors& t, const TreePlan& pl, hipStream_t st) {
 #define RATTN_TREE(CT_, KG_, NW_)                                                                   \
   if (pl.CT == CT_ && pl.KG == KG_ && pl.NW == NW_) {                                               \
-    if constexpr (NW_ == 8) {                                                                       \
+    if constexpr (KG_ == 8) {   /* (the others have too many work-groups to share keys) */          \
       if (td.workspace && pl.nsplit > 1) {                                                          \
         launch_tree<IO, RT, D, CT_, KG_, NW_, true>(td, t, pl, st);                                 \
         return;                                                                                     \

@@ -22,7 +22,8 @@ int main() {
   float* fx = (float*)x;
   const int shapes[][5] = {{1, 1, 1, 64, 1},       {1, 16, 4, 128, 512},   {128, 32, 8, 128, 512}, {65535, 1, 1, 128, 9},
                            {1, 65535, 65535, 64, 3}, {1, 4, 1, 128, 1 << 30}, {7, 320, 1, 64, 1000}, {3, 65535, 1, 128, 70000},
-                           {1, 4, 1, 64, 0x7fffffff}, {24, 40, 8, 128, 2048}, {400, 8, 2, 64, 300}};
+                           {1, 4, 1, 64, 0x7fffffff}, {24, 40, 8, 128, 2048}, {400, 8, 2, 64, 300}, {2, 8, 2, 128, 320}, {3, 8, 2, 128, 4096},
+                           {16, 20, 4, 64, 1500}};
   for (auto& s : shapes)
     for (int dtype = 0; dtype < 2; ++dtype)
       for (int nodes : {1, 2, 3, 16, 17, 33, 63, 64})
@@ -38,6 +39,7 @@ int main() {
           const int rows = nodes * td.G, per = pl.NW / pl.KG * 16 * pl.CT;
           CHECK(pl.CT >= 1 && pl.KG >= 1 && pl.NW % pl.KG == 0 && pl.nsplit >= 1 && pl.nsplit <= 128);
           CHECK((long long)pl.blocks * per >= rows && (long long)(pl.blocks - 1) * per < rows);
+          CHECK(pl.nsplit == 1 || (pl.KG == 8 && pl.NW == 8));   // the forms in which work-groups share keys
           // a launch's grid, and a ticket and the partial sums for every work-group
           const long long grid = ((long long)td.N * td.Hkv + 7) / 8 * 8 * pl.blocks * pl.nsplit;
           CHECK(grid < (1ll << 31));

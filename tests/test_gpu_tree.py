@@ -332,6 +332,65 @@ def test_workspace_contents_do_not_matter_and_without_one():
     assert bool(((o.float() - ref.float()).abs() <= 2 * 2.0 ** -8 * ref.float().abs() + 1e-3).all())
 
 
+@pytest.mark.parametrize("M,G,W", [(1, 4, 2048), (13, 3, 2048), (64, 4, 4096)])
+def test_workspaces_of_the_asked_size(M, G, W):
+    """Steps whose work-groups share keys write nothing around a workspace of just the bytes that are asked for."""
+    N, Hkv, D, B = 2, 2, 128, 4096
+    x = make(N, M, G * Hkv, Hkv, D, W, "bf16", [2 * W, W + 7], True, 8050, 2)
+    P = lambda t: None if t is None else t.data_ptr()
+    n, m = ctypes.c_size_t(), ctypes.c_size_t()
+    p = rb.RattnTreeParams(N, G * Hkv, Hkv, D, W, rb.RATTN_BF16, M, 0.1, 1e-6, 0)
+    d = rb.RattnDecodeParams(N, G * Hkv, Hkv, D, W, rb.RATTN_BF16, 0.1, 1e-6, 0)
+    assert rb.lib().rattn_tree_workspace_bytes(ctypes.byref(p), 1, ctypes.byref(n)) == 0 and n.value > 0
+    assert rb.lib().rattn_decode_packed_workspace_bytes(ctypes.byref(d), ctypes.byref(m)) == 0 and m.value > 0
+    ref, o = step(x, 0.1), torch.empty_like(x["q"])
+    full = torch.full((n.value + 2 * B,), 0xA5, dtype=torch.uint8, device="cuda")
+    assert rb.lib().rattn_tree_step(ctypes.byref(p), *(P(x[t]) for t in ("q", "k", "v", "parent")), None, P(x["pos"]), P(x["kr"]), P(x["ks"]), P(x["vr"]),
+                                    P(x["vs"]), P(x["state"]), P(x["gs"]), P(x["gr"]), P(o), full.data_ptr() + B, n.value, rb._stream()) == 0
+    assert torch.equal(o, ref) and bool((full[:B] == 0xA5).all()) and bool((full[B + n.value:] == 0xA5).all())
+    q, k, v = (x[t][:, 0].contiguous() for t in "qkv")
+    y = {t: x[t].clone() for t in CACHE}
+    ref = rb.rattn_decode_step_packed(q, k, v, x["pos"], *(y[t] for t in ("kr", "ks", "vr", "vs", "state")), x["gs"], x["gr"], softmax_scale=0.1)
+    o, full = torch.empty_like(q), torch.full((m.value + 2 * B,), 0xA5, dtype=torch.uint8, device="cuda")
+    assert rb.lib().rattn_decode_step_packed(ctypes.byref(d), P(q), P(k), P(v), P(x["pos"]), P(x["kr"]), P(x["ks"]), P(x["vr"]), P(x["vs"]), P(x["state"]),
+                                             P(x["gs"]), P(x["gr"]), P(o), full.data_ptr() + B, m.value, rb._stream()) == 0
+    assert torch.equal(o, ref) and bool((full[:B] == 0xA5).all()) and bool((full[B + m.value:] == 0xA5).all())
+    assert all(torch.equal(x[t].view(torch.uint8), y[t].view(torch.uint8)) for t in CACHE)
+
+
+def test_steps_of_two_streams_at_once():
+    """Steps that share keys among work-groups, on two streams that run at the same time, each with workspaces of its own."""
+    N, M, Hq, Hkv, D, W = 2, 9, 8, 2, 128, 2048
+    xs = [make(N, M, Hq, Hkv, D, W, "bf16", [3 * W, W + 1], packed, 8060 + packed, 2) for packed in (False, True)]
+    refs = [step(x, 0.1) for x in xs]
+    heads = [tuple(x[n][:, 0].contiguous() for n in "qkv") for x in xs]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in xs], [[], []]
+    for _ in range(20):
+        for i, x in enumerate(xs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(step(x, 0.1))
+    torch.cuda.synchronize()
+    for i, ref in enumerate(refs):
+        assert all(torch.equal(o, ref) for o in got[i])
+    caches = [{n: xs[1][n].clone() for n in CACHE} for _ in range(3)]
+
+    def decode(y):
+        return rb.rattn_decode_step_packed(*heads[1], xs[1]["pos"], y["kr"], y["ks"], y["vr"], y["vs"], y["state"], softmax_scale=0.1)
+
+    want = [decode(caches[2]) for _ in range(5)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(decode(caches[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want))
+        assert all(torch.equal(caches[i][n].view(torch.uint8), caches[2][n].view(torch.uint8)) for n in CACHE)
+
+
 @pytest.mark.parametrize("W", [64, 2048])
 def test_captured_and_on_another_stream(W):
     """A step and a commit in one graph, replayed with eager work between the replays; two graphs that share one workspace pool are
