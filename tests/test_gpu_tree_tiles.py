@@ -33,7 +33,8 @@ SHAPES = [  # N, M, Hq, Hkv, W, spread: pairs * ceil(M G / 64) above 512
     (130, 64, 4, 2, 20, 1),              # chains longer than the window
     (27, 64, 20, 1, 96, 5),              # 20 query heads of a KV head: gains from memory
     (520, 64, 2, 1, 1, 2),               # a window of one
-    (65, 24, 32, 8, 64, 4)]              # 96 rows, a window of one tile
+    (65, 24, 32, 8, 64, 4),              # 96 rows, a window of one tile
+    (40, 33, 40, 8, 130, 3), (64, 33, 32, 8, 50, 1)]   # more work-groups than run at once, of 64 sequences at most: the longest first
 
 
 @pytest.mark.parametrize("packed", [False, True])
@@ -98,11 +99,12 @@ def test_without_gains_and_gains_of_any_alignment():
     assert torch.equal(step({**x, **odd}, 0.1), ref)
 
 
-def test_counts_and_sequences_without_work():
-    N, M, W = 132, 19, 33
+@pytest.mark.parametrize("N,M,Hkv", [(132, 19, 2), (48, 40, 8)])
+def test_counts_and_sequences_without_work(N, M, Hkv):
+    W = 33
     pos = positions(N, W)
     pos[9], pos[17] = -1, -5
-    x = make(N, M, 8, 2, 128, W, "bf16", pos, False, 9500, 3)
+    x = make(N, M, 4 * Hkv, Hkv, 128, W, "bf16", pos, False, 9500, 3)
     count = [(M, 0, 4, -2, 17, 1, M + 5, 8)[i % 8] for i in range(N)]
     for name in ("q", "k", "v"):                 # what stands behind the last node is no number
         for n, c in enumerate(count):
