@@ -589,8 +589,8 @@ def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None,
     """The layer for a tree of up to 64 drafted tokens behind each of N sequences; rings and state are only read.
 
     q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M]: the earlier node that a node continues, -1 = the sequence's last token;
-    pos int32 [N]: tokens in the cache; count int32 [N]: nodes of each sequence (None: M), rows behind them are left as they are
-    in `out` (zero where it is allocated here).  k_scale, v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
+    pos int32 [N]: tokens in the cache; count int32 [N]: nodes of each sequence (None: M); rows behind them, and all of a
+    sequence with pos < 0, are left as they are in `out` (zero where it is allocated here and count given).  k_scale, v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
     o = _native.tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa, gamma_rla, softmax_scale, rms_eps, count, k_scale,
                           v_scale, out, feature_map)
     if o is not None:

@@ -44,7 +44,7 @@ __device__ __forceinline__ void buf_store(rsrc_t r, f32x4_t v, int off) {
 // bf16: 32 keys, 16x16x32 tiles; fp32: 16 keys, 16x16x4 tiles (exact fp32 products and sums).
 template <typename IO, typename RT, int D, bool ONCE> struct RingSet;
 
-  // x as three bf16 terms of 8 bits, together exact; x is left with what they leave
+// x as three bf16 terms of 8 bits, together exact; x is left with what they leave
 __device__ __forceinline__ void three_terms(float (&x)[8], bf16x8_t (&term)[3]) {
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
@@ -55,15 +55,15 @@ __device__ __forceinline__ void three_terms(float (&x)[8], bf16x8_t (&term)[3]) 
     for (int i = 0; i < 8; ++i) x[i] -= t[i];  // exact
   }
 }
-// acc[e] += V^T P^T for feature EV*r16 + e of each lane's piece; two rows are interleaved per dword with v_perm_b32.  The
-  // fp32 probabilities pass through the bf16 tiles as three terms of 8 bits whose products share one accumulator, which is
-  // as good as fp32 products with the bf16 values (one term: 1.12 - 1.16 times the error of the output against fp64,
-  // which is mostly the output's own rounding).  The extra products hide behind the rings: 24 x 8 KV heads, W = 2048, 39.9 us
-  // either way; one sequence, where they are part of the chain, 11.2 us against 10.8.
-  __device__ __forceinline__ void prob_terms(const f32x4_t (&p)[2], bf16x8_t (&pop)[3]) {
+// The fp32 probabilities pass through the bf16 tiles as three terms of 8 bits whose products share one accumulator, which is
+// as good as fp32 products with the bf16 values (one term: 1.12 - 1.16 times the error of the output against fp64,
+// which is mostly the output's own rounding).  The extra products hide behind the rings: 24 x 8 KV heads, W = 2048, 39.9 us
+// either way, packed 25.5 against 25.2 with two terms; one sequence, where they are part of the chain, 11.2 us against 10.8.
+__device__ __forceinline__ void prob_terms(const f32x4_t (&p)[2], bf16x8_t (&pop)[3]) {
   float r[8] = {p[0][0], p[0][1], p[0][2], p[0][3], p[1][0], p[1][1], p[1][2], p[1][3]};
   three_terms(r, pop);
 }
+// acc[e] += V^T P^T for feature EV*r16 + e of each lane's piece; two rows are interleaved per dword with v_perm_b32
 template <int EV, typename ROW>
 __device__ __forceinline__ void accumulate_bf16(const ROW (&v)[8], const bf16x8_t (&pop)[3], f32x4_t* acc) {
 #pragma unroll
