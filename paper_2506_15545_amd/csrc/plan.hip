@@ -156,12 +156,13 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   const int rows = td.M * td.G, keys = dtype == 0 ? 16 : 32, pieces = td.D / keys + 1;
   const int sets = (int)((td.W + (keys - 1ll)) / keys) + (td.M + keys - 1) / keys;
   const long long pairs = (long long)td.N * td.Hkv;
-  // Keys through LDS where waves that fetch them themselves would be more than the chip holds at once (work-groups of 64 rows, one
-  // per CU).  us, direct | tiles, bf16, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.9 | 34.8, 57.8 | 68.2; of 256 46.2 | 37.3,
-  // 107 | 72; 128 of 128 rows 26.3 | 35.1, 59.2 | 69.3; 192 of 96 42.6 | 34.9, 107 | 72; 64 of 256 26.3 | 36.1, 53.5 | 69.3; of 512
-  // 44.1 | 38.5, 102 | 71.  D = 64: 64 of 256 16.4 | 22.4, 36.3 | 48.0; of 512 28.9 | 23.7, 66.6 | 49.3
-  // (packed: 64 of 256 rows, W = 2048 66 | 49).  Packed rings of D = 128, which they unpack on the way (at the cost of registers), from
-  // twice as many on: 192 of 128 42.1 | 47.6, 104 | 123; 320 of 128 62 | 64, 153 | 143; 128 of 512 82 | 61, 201 | 141
+  // Keys through LDS where waves that fetch them themselves would be more than the chip holds at once (work-groups of 64 rows, one per
+  // CU).  us, direct | tiles, bf16, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.9 | 34.8, 57.8 | 68.2; of 256 46.2 | 37.3, 107 |
+  // 72; 128 of 128 rows 25.6 | 34.2, 58.6 | 69.1; 136 of 128 42.5 | 34.2, 104 | 69; 192 of 96 42.6 | 34.9, 107 | 72; 64 of 256 26.3 |
+  // 36.1, 53.5 | 69.3; of 512 44.1 | 38.5, 102 | 71.  D = 64: 64 of 256 16.4 | 22.4, 36.3 | 48.0; of 512 28.9 | 23.7, 66.6 | 49.3
+  // (packed: 16.0 | 24.4, 38.4 | 59.6; of 512 29.0 | 26.3, 72 | 61).  Packed rings of D = 128, which they unpack on the way (at the cost
+  // of registers), from twice as many on: 192 of 128 42.1 | 47.6, 104 | 123; 320 of 128 62 | 64, 153 | 143; 128 of 512 82 | 61, 201 |
+  // 141
   if (dtype == 1 && rows > 64 && pairs * ((rows + 63) / 64) > (packed && td.D == 128 ? 512 : 256)) {
     p.tiles = 1;
     p.CT = 2;

@@ -6,9 +6,9 @@
 // layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
 // second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
 // phi(k) of the keys that leave, then the state, both as two bf16 terms.
-// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 91 us, 397 TFLOP/s; fetching their
-// own keys the waves take 164.  Bound by the operands from LDS (a wave reads all of a tile for its 32 rows: 2.1 of 4.2 k
-// cycles that the eight waves of a CU take for a tile each) and by the products and exponentials around them (2.0 and 1.6 k).
+// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 82 us, 440 TFLOP/s; fetching their
+// own keys the waves take 164.  Bound by the operands from LDS (a wave reads all of a tile for its 32 rows: 2.1 of some
+// 3.8 k cycles that the eight waves of a CU take for a tile each) and by the products and exponentials around them (2.0 and 1.6 k).
 #pragma once
 #include "tree_group.hpp"
 
@@ -328,8 +328,11 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
         for (int ct = 0; ct < NCT; ++ct) acc[ct] *= alpha;
       }
       // The second products in explicit order: a half's operands are read while the half before is worked on, the second half's
-      // exponentials stand between the first one's products (left to the compiler: 8 % more at W = 2048).  (One bf16 term for the
-      // probabilities, as in the layer's forward: the output's own rounding is as large.)
+      // exponentials stand between the first one's products (left to the compiler: 8 % more at W = 2048).  Of the two waves of a SIMD
+      // the one that is here goes first, so that the other's first products fill what it leaves: 91 -> 82 us (the first products
+      // preferred as well 85, they alone 86).  (One bf16 term for the probabilities, as in the layer's forward: the output's
+      // own rounding is as large.)
+      __builtin_amdgcn_s_setprio(1);
       constexpr int NP = 2 * NCT;
       bf16x8_t v[NP], pw[2];
       float pr[16];
@@ -355,6 +358,7 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
       pw[1] = pack_bf16x8(pr + 8);
 #pragma unroll
       for (int i = 0; i < NP; ++i) acc[i % NCT] = mfma32(v[i], pw[i / NCT], acc[i % NCT]);
+      __builtin_amdgcn_s_setprio(0);
     }
     if (PACKED && !live && t + 1 < ntile) half_way(t + 1, buf ^ 1);
     if (t + 1 < ntile) deliver(t + 1, buf ^ 1);
