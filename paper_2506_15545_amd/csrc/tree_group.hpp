@@ -125,25 +125,28 @@ template <int D, bool PERM, int CT> struct TreeMath<bf16_t, D, PERM, CT> {
     }
   }
 
-  // a set of rows in the tensors' type: keys at `stride` bytes
+  // a set of rows in the tensors' type: keys at `stride` bytes.  (The rows' offsets are part of each lane's, which is what a resource's
+  // size is compared with: rows behind the last one read as zero)
   struct Plain {
     Row k[2];
     vrow_t v[8];
     __device__ __forceinline__ void load_k(rsrc_t rows, int stride, int r16, int q4) {
       const int off = opaque(stride * r16 + 2 * piece_feature<PERM>(0, q4));
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < 2; ++c) {
+        const int offc = off + 16 * stride * c;
 #pragma unroll
         for (int j = 0; j < J; ++j)
-          k[c].op[j] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rows, off + 2 * piece_feature<PERM>(j, 0), 16 * stride * c, 0));
+          k[c].op[j] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offc + 2 * piece_feature<PERM>(j, 0), 0, 0));
+      }
     }
     __device__ __forceinline__ void load_v(rsrc_t rows, int stride, int r16, int q4) {
       const int off = opaque(4 * stride * q4 + 2 * EV * r16);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int row = (u < 4 ? 0 : 16) + (u & 3);
-        if constexpr (EV == 8) v[u] = __builtin_bit_cast(vrow_t, __builtin_amdgcn_raw_buffer_load_b128(rows, off, stride * row, 0));
-        else v[u] = __builtin_bit_cast(vrow_t, __builtin_amdgcn_raw_buffer_load_b64(rows, off, stride * row, 0));
+        const int offu = off + stride * ((u < 4 ? 0 : 16) + (u & 3));
+        if constexpr (EV == 8) v[u] = __builtin_bit_cast(vrow_t, __builtin_amdgcn_raw_buffer_load_b128(rows, offu, 0, 0));
+        else v[u] = __builtin_bit_cast(vrow_t, __builtin_amdgcn_raw_buffer_load_b64(rows, offu, 0, 0));
       }
     }
     __device__ __forceinline__ void key_row(int c, Row& r) const { r = k[c]; }
@@ -377,7 +380,7 @@ template <int D, bool PERM, int CT> struct TreeMath<float, D, PERM, CT> {
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int hf = 0; hf < D / 64; ++hf)
-          this->v[i][hf] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, off + 256 * hf, stride * i, 0));
+          this->v[i][hf] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rows, off + stride * i + 256 * hf, 0, 0));
     }
   };
   struct Packed : Base {

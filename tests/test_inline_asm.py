@@ -18,3 +18,30 @@ def test_inline_assembly_holds_nothing_but_loads_into_lds():
     assert sum(bool(t) for _, t in texts) == 2    # the two forms of the load
     for name, text in texts:
         assert not text or LDS_LOAD.fullmatch(text), f"{name}: {text}"
+
+
+def arguments(text, at):
+    """The arguments of the call whose opening bracket is text[at], split at its own commas."""
+    depth, start, out = 0, at + 1, []
+    for i in range(at, len(text)):
+        depth += text[i] in "([{"
+        depth -= text[i] in ")]}"
+        if depth == 0 or (depth == 1 and text[i] == ","):
+            out.append(text[start:i].strip())
+            start = i + 1
+        if depth == 0:
+            return out
+
+
+def test_buffer_accesses_have_no_scalar_offset():
+    """The end of a ring or of the drafted tokens is enforced by a buffer resource's size, and only the offset that a lane has of its
+    own is sure to be compared with it: where the scalar offset is taken off the size, one that is larger leaves no end at all."""
+    found = 0
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.h*p"))):
+        text = re.sub(r"//[^\n]*", "", open(path).read())
+        for m in re.finditer(r"__builtin_amdgcn_raw_buffer_(load|store)_\w+\(", text):
+            args = arguments(text, m.end() - 1)
+            assert len(args) == (4 if m.group(1) == "load" else 5), (path, args)
+            assert args[-2] == "0", (os.path.basename(path), m.group(0), args)
+            found += 1
+    assert found >= 10
