@@ -157,12 +157,12 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   const int sets = (int)((td.W + (keys - 1ll)) / keys) + (td.M + keys - 1) / keys;
   const long long pairs = (long long)td.N * td.Hkv;
   // Keys through LDS where waves that fetch them themselves would be more than the chip holds at once (work-groups of 64 rows, one per
-  // CU).  us, direct | tiles, bf16, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.9 | 34.8, 57.8 | 68.2; of 256 46.2 | 37.3, 107 |
-  // 72; 128 of 128 rows 25.6 | 34.2, 58.6 | 69.1; 136 of 128 42.5 | 34.2, 104 | 69; 192 of 96 42.6 | 34.9, 107 | 72; 64 of 256 26.3 |
-  // 36.1, 53.5 | 69.3; of 512 44.1 | 38.5, 102 | 71.  D = 64: 64 of 256 16.4 | 22.4, 36.3 | 48.0; of 512 28.9 | 23.7, 66.6 | 49.3
-  // (packed: 16.0 | 24.4, 38.4 | 59.6; of 512 29.0 | 26.3, 72 | 61).  Packed rings of D = 128, which they unpack on the way (at the cost
-  // of registers), from twice as many on: 192 of 128 42.1 | 47.6, 104 | 123; 320 of 128 62 | 64, 153 | 143; 128 of 512 82 | 61, 201 |
-  // 141
+  // CU).  us, direct | tiles, bf16, full rings, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.7 | 38.5, 57.0 | 78.9; of 256
+  // 47.9 | 42.2, 107 | 84; 128 of 128 rows 26.1 | 38.8, 60.4 | 81.2; 136 of 128 44.7 | 39.3, 106 | 80; 192 of 96 45.0 | 39.3, 108 |
+  // 81; 64 of 256 28.5 | 40.9, 57.3 | 82.1; of 512 50.7 | 45.0, 108 | 87.  D = 64: 64 of 256 17.0 | 26.6, 35.6 | 57.2; of 512 31.1 |
+  // 28.8, 69.3 | 61.3 (packed: 17.4 | 29.7, 39.7 | 70.4; of 512 31.4 | 31.9, 73.9 | 72.0).  Packed rings of D = 128, which they unpack
+  // on the way (at the cost of registers), from twice as many on: 192 of 128 45.5 | 48.2, 104 | 111; 256 of 128 48.6 | 49.8, 108 | 115;
+  // 320 of 128 66.1 | 63.7, 155 | 135; 96 of 256 47.4 | 48.0, 101 | 107; 128 of 512 93.5 | 67.8, 212 | 144
   if (dtype == 1 && rows > 64 && pairs * ((rows + 63) / 64) > (packed && td.D == 128 ? 512 : 256)) {
     p.tiles = 1;
     p.CT = 2;

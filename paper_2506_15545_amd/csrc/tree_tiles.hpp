@@ -6,9 +6,10 @@
 // layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
 // second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
 // phi(k) of the keys that leave, then the state, both as two bf16 terms.
-// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 82 us, 440 TFLOP/s; fetching their
-// own keys the waves take 164.  Bound by the operands from LDS (a wave reads all of a tile for its 32 rows: 2.1 of some
-// 3.8 k cycles that the eight waves of a CU take for a tile each) and by the products and exponentials around them (2.0 and 1.6 k).
+// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 99 us, 365 TFLOP/s; fetching their
+// own keys the waves take 164.  Bound by the way of a wave through its tiles (products, masks and exponentials, products): the
+// work-groups with full rings, less than half of all, are about one for each CU, and the rest waits for them.  Over the whole launch
+// the matrix units are busy for 27 % of it, the vector units for 38 %, LDS for 12 %.
 #pragma once
 #include "tree_group.hpp"
 
@@ -22,8 +23,8 @@ constexpr int TILE_WAVES = TREE_TILE_WAVES, TILE_THREADS = 64 * TILE_WAVES;
 // with the rest of the inputs, where the end of a work-group waited for them (13 k of 196 k cycles)
 constexpr int TILE_GAINS = 8;
 // More work-groups than run at once (two on each of 256 CUs) take the sequences with the longest rings first: one that starts when
-// others end is a short one.  (24 sequences of 100 to 4000 tokens, 8 KV heads, 305 rows, W = 2048: 96 us in order,
-// 91 so; then the longest work-groups are what the rest waits for.)
+// others end is a short one.  (24 sequences of 100 to 4000 tokens, 8 KV heads, 305 rows, W = 2048, when a work-group took less:
+// 96 us in order, 91 so; then the longest work-groups are what the rest waits for.)
 constexpr unsigned TILE_AT_ONCE = 512;
 template <int D> constexpr size_t tree_tile_lds() { return 4 * (size_t)TileGeom<D>::KT + 2 * TILE_GAINS * D * 4; }
 
@@ -151,14 +152,15 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
   const DmaLane<D> dma_lane = make_dma_lane<D>(lane, D);
   auto request_codes = [&](int t, const RT* ring, const uint8_t* scales) {
     if constexpr (PACKED) {
-      const int base = ring_base(t);
+      const int base = ring_base(t), last = nvalid - 1 - base;
+      const uint8_t *rc = reinterpret_cast<const uint8_t*>(ring) + (size_t)base * D, *rs = scales + (size_t)base * SB;   // (scalar)
 #pragma unroll
       for (int i = 0; i < PT; ++i) {
         const int x = threadIdx.x + i * TILE_THREADS;
         if (x < PK) {
-          const size_t r = (size_t)min(base + x / (CH / 2), nvalid - 1), c = x % (CH / 2);
-          codes[i] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const uint8_t*>(ring) + r * D + 16 * c);
-          code_scale[i] = scales[r * SB + c / 2];
+          const unsigned r = min(x / (CH / 2), last), c = x % (CH / 2);
+          codes[i] = *reinterpret_cast<const u32x4_t*>(rc + (r * D + 16 * c));
+          code_scale[i] = rs[r * SB + c / 2];
         }
       }
     }
@@ -327,37 +329,54 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) acc[ct] *= alpha;
       }
-      // The second products in explicit order: a half's operands are read while the half before is worked on, the second half's
-      // exponentials stand between the first one's products (left to the compiler: 8 % more at W = 2048).  Of the two waves of a SIMD
-      // the one that is here goes first, so that the other's first products fill what it leaves: 91 -> 82 us (the first products
-      // preferred as well 85, they alone 86).  (One bf16 term for the probabilities, as in the layer's forward: the output's
-      // own rounding is as large.)
+      // The second products in explicit order: operands are read four products ahead, the second half's exponentials stand between
+      // the first half's products.  Of the two waves of a SIMD the one that is here goes first, so that the other's first products
+      // fill what it leaves (108 -> 99 us).
+      // Two bf16 terms for the probabilities, as in the direct kernel, so that a sequence's result does not get worse in a larger
+      // batch: with one the output is off by 2.1e-3 of its norm, with two by the 1.66e-3 of its own rounding (81 | 99 us).
       __builtin_amdgcn_s_setprio(1);
-      constexpr int NP = 2 * NCT;
-      bf16x8_t v[NP], pw[2];
+      constexpr int NP = 2 * NCT, AHEAD = 4;   // products of a half, operands that are read ahead
+      bf16x8_t v[AHEAD], ph[2], pl[2];
       float pr[16];
-      auto operand = [&](int h, int i) { return tile_trp<D>(V, lo, 32 * h + 16 * (i / NCT), i % NCT); };
+      auto read = [&](int x) {
+        const int i = x % NP;
+        v[x % AHEAD] = tile_trp<D>(V, lo, 32 * (x / NP) + 16 * (i / NCT), i % NCT);
+      };
       auto prob = [&](int h, int i) { pr[i] = fast_exp2(__builtin_fmaf(s[h][i], sc, -m)); lsum[i & 3] += pr[i]; };
+      auto terms = [&]() {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) v[i] = operand(0, i);
+        for (int k = 0; k < 2; ++k) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = pr[8 * k + i];
+          split2(x, ph[k], pl[k]);
+        }
+      };
+      auto product = [&](int x) {
+        f32x16_t& o = acc[x % NCT];
+        o = mfma32(v[x % AHEAD], pl[x % NP / NCT], o);
+        o = mfma32(v[x % AHEAD], ph[x % NP / NCT], o);
+        if (x + AHEAD < 2 * NP) read(x + AHEAD);
+      };
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) read(x);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < 16; ++i) prob(0, i);
-      pw[0] = pack_bf16x8(pr);
-      pw[1] = pack_bf16x8(pr + 8);
+      terms();
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        acc[i % NCT] = mfma32(v[i], pw[i / NCT], acc[i % NCT]);
+      for (int x = 0; x < NP; ++x) {
+        product(x);
 #pragma unroll
-        for (int j = 16 / NP * i; j < 16 / NP * (i + 1); ++j) prob(1, j);
-        v[i] = operand(1, i);
+        for (int j = 16 / NP * x; j < 16 / NP * (x + 1); ++j) prob(1, j);
         __builtin_amdgcn_sched_barrier(0);
       }
-      pw[0] = pack_bf16x8(pr);
-      pw[1] = pack_bf16x8(pr + 8);
+      terms();
 #pragma unroll
-      for (int i = 0; i < NP; ++i) acc[i % NCT] = mfma32(v[i], pw[i / NCT], acc[i % NCT]);
+      for (int x = NP; x < 2 * NP; ++x) {
+        product(x);
+      }
       __builtin_amdgcn_s_setprio(0);
     }
     if (PACKED && !live && t + 1 < ntile) half_way(t + 1, buf ^ 1);
