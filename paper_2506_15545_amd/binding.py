@@ -590,7 +590,8 @@ def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None,
 
     q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M]: the earlier node that a node continues, -1 = the sequence's last token;
     pos int32 [N]: tokens in the cache; count int32 [N]: nodes of each sequence (None: M); rows behind them, and all of a
-    sequence with pos < 0, are left as they are in `out` (zero where it is allocated here and count given).  k_scale, v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
+    sequence with pos < 0, are left as they are in `out` (zero where it is allocated here, which costs a pass over it).  k_scale,
+    v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
     o = _native.tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa, gamma_rla, softmax_scale, rms_eps, count, k_scale,
                           v_scale, out, feature_map)
     if o is not None:
@@ -604,7 +605,7 @@ def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None,
     p, nbytes = _tree_plan(k.shape, Hq, W, k.dtype, k_scale is not None, float(softmax_scale), float(rms_eps), feature_map)
     gs, gr = _gain(gamma_swa, Hq, D, q.device), _gain(gamma_rla, Hq, D, q.device)
     if out is None:
-        o = torch.empty_like(q) if count is None else torch.zeros_like(q)
+        o = torch.zeros_like(q)
     else:
         o = _check_out(out, q)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=q.device) if nbytes else None

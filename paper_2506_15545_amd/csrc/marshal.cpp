@@ -369,7 +369,7 @@ PyObject* do_tree_step(PyObject* const* args) {
   r.p.rms_eps = (float)PyFloat_AS_DOUBLE(args[11]);
   THPObjectPtr result;
   void* o;
-  if (!output(args[15], *q, r.dev, count != nullptr, result, o)) {
+  if (!output(args[15], *q, r.dev, true, result, o)) {   // (zero: a sequence may have rows, or nothing, without work)
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
   }

@@ -4,6 +4,7 @@ order, which gives other bits)."""
 import pytest
 import torch
 
+from paper_2506_15545_amd import binding as rb
 from test_gpu_tree import make, step
 
 pytestmark = pytest.mark.gpu
@@ -65,3 +66,23 @@ def test_many_rows(D, packed):
     x = make(N, M, 8, 2, D, W, "bf16", [(33, 200)[i % 2] for i in range(N)], packed, 8600, 2)
     zero, nan = both(x, 0.1)
     assert bool(torch.isfinite(zero).all()) and torch.equal(zero, nan)
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("N,M", [(3, 6), (260, 17)])
+@pytest.mark.parametrize("counts", [True, False])
+def test_sequences_without_work_are_zero_in_a_new_output(counts, N, M, native, monkeypatch):
+    """Whatever the memory held that the output is made of: a sequence with pos < 0 is zero, as are the rows behind a count."""
+    if not native:
+        monkeypatch.setattr(rb._native, "tree_step", rb._no_native, raising=False)
+    x = make(N, M, 8, 2, 128, 40, "bf16", [(70, -1, 20)[i % 3] for i in range(N)], False, 8700, 2)
+    count = torch.full((N,), M - 2, dtype=torch.int32, device="cuda") if counts else None
+    idle = torch.arange(N) % 3 == 1
+    torch.cuda.synchronize()
+    for _ in range(3):
+        left = torch.full_like(x["q"], float("nan"))     # goes back to the allocator, which hands it out next
+        del left
+        o = step(x, 0.1, count=count)
+        assert bool((o[idle] == 0).all()) and bool(torch.isfinite(o).all()) and bool((o[~idle][:, : M - 2] != 0).any())
+        if counts:
+            assert bool((o[:, M - 2:] == 0).all())
