@@ -248,7 +248,9 @@ typedef struct {
 
 /* The layer for node i < count[n] of every sequence n with pos[n] = p tokens in its cache: node i is the token at position
  * p + (its depth), behind the cache's tokens and its own ancestors, and sees nothing of other branches.  With one node this is
- * what rattn_decode_step returns for it.
+ * what rattn_decode_step (over packed rings rattn_decode_step_packed) returns for it.  Deeper nodes see their ancestors as they are
+ * given, also where the rings are packed: decode steps would have stored those in 8 bits first, so that over packed rings the nodes
+ * below the first ones differ from a chain of rattn_decode_step_packed by what that rounding changes (2^-4 of a feature at most).
  *   q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M] (device): parent[n,i] < i is the node that i continues, -1 the
  *     sequence's last token (any other value counts as -1)
  *   count int32 [N] (device), NULL = M for all: nodes of each sequence; rows of o behind them are left as they are.  A sequence
@@ -267,7 +269,10 @@ rattn_status rattn_tree_step(const rattn_tree_params* p, const void* q, const vo
 
 /* accepted[n] (int32 [N], device) is the last accepted node of sequence n; it and its ancestors, L of them, become tokens
  * p .. p + L - 1: keys and values that leave the window are folded into the state (which is read only if p > W, and left as it is
- * while nothing leaves), the others take their slots, packed where the rings are.  accepted[n] outside 0 .. M-1 or pos[n] < 0: the
+ * while nothing leaves), the others take their slots, packed where the rings are.  The rings are to the bit what L decode steps
+ * leave.  So is the state but for the order of rounding, with one exception: of a path longer than a packed window the first L - W
+ * tokens leave without ever having had a slot and are folded in as given, where rattn_decode_step_packed would have folded their 8
+ * bits (in one commit of 2 W tokens thus W more of them as given than in two of W).  accepted[n] outside 0 .. M-1 or pos[n] < 0: the
  * sequence's cache stays as it is.  pos is not written: the caller advances it by L when every layer is done.
  * (softmax_scale and rms_eps are not used but must be valid.) */
 rattn_status rattn_tree_commit(const rattn_tree_params* p, const void* k, const void* v, const int32_t* parent,

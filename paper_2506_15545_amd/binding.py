@@ -591,7 +591,8 @@ def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None,
     q [N,M,Hq,D]; k, v [N,M,Hkv,D]; parent int32 [N,M]: the earlier node that a node continues, -1 = the sequence's last token;
     pos int32 [N]: tokens in the cache; count int32 [N]: nodes of each sequence (None: M); rows behind them, and all of a
     sequence with pos < 0, are left as they are in `out` (zero where it is allocated here, which costs a pass over it).  k_scale,
-    v_scale: of packed rings (rattn_ring_pack).  Returns o [N,M,Hq,D]."""
+    v_scale: of packed rings (rattn_ring_pack).  A node sees its ancestors as given, also over packed rings, where decode steps would
+    have stored them in 8 bits first.  Returns o [N,M,Hq,D]."""
     o = _native.tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa, gamma_rla, softmax_scale, rms_eps, count, k_scale,
                           v_scale, out, feature_map)
     if o is not None:
@@ -617,7 +618,8 @@ def rattn_tree_step(q, k, v, parent, pos, k_ring, v_ring, state, gamma_swa=None,
 def rattn_tree_commit(k, v, parent, accepted, pos, k_ring, v_ring, state, k_scale=None, v_scale=None, feature_map="softmax"):
     """The accepted node of each sequence's tree and its ancestors become tokens of the cache: rings (packed where scales are
     given) and state are updated in place.  accepted int32 [N]: node, or -1 for none.  pos is left to the caller, who advances it by
-    the length of the accepted path when every layer is done."""
+    the length of the accepted path when every layer is done.  Of a path longer than a packed window the tokens that leave at once are
+    folded into the state as given, not as 8 bits."""
     r = _native.tree_commit(k, v, parent, accepted, pos, k_ring, v_ring, state, k_scale, v_scale, feature_map)
     if r is not None:
         if r.__class__ is int:

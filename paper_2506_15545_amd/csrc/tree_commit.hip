@@ -4,7 +4,8 @@
 // leaving tokens had.  Where L > W the first of the path leave at once.
 // One work-group per (sequence, KV head): the leaving rows as phi(k) and v in LDS, then the slots are free; a thread holds 4 x 4
 // tiles of the state, requested before anything else, and adds the L outer products in the order of the tokens, in fp32 fused
-// multiply-adds (L of them per entry of the state, which decode steps would have added one by one in the same order).
+// multiply-adds (L of them per entry of the state, which decode steps would have added one by one in the same order).  Over packed
+// rings the tokens that leave at once (L > W) are folded in as given, where decode steps would have stored them in 8 bits first.
 // Bound: HBM, the state once in and once out.  128 sequences of 8 KV heads, D = 128, paths of up to 6 tokens, packed rings of 512 slots:
 // 19 us, 7 TB/s (a part of the state from the last-level cache); one sequence of 4 KV heads 4.4 us, a launch and three trips to memory.
 #include "packed.hpp"
