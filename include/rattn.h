@@ -212,7 +212,8 @@ rattn_status rattn_prefill_chunk(const rattn_params* p, int32_t pos0, const void
  * D/32 scale bytes; byte b of a block of 32 features is the factor 2^(b-127) (E8M0, b from 1 on).  The factor is the least
  * one with which the largest finite feature of the block is at most 448, the numbers are the nearest ones (ties to even), so
  * a stored feature is off by at most 2^-4 of itself, or by 2^-10 times the factor.  Infinities and NaN are stored as NaN.  What
- * is stored is exact in bf16 and fp32, and packing what was unpacked gives the same values.
+ * is stored is exact in fp32, and in bf16 but for values below 2^-130 that are no multiple of its least step, 2^-133: those are the
+ * nearest multiple.  Packing what was unpacked gives the values that were unpacked.
  *   codes [N,Hkv,W,D], scales [N,Hkv,W,D/32], one byte each, 16-byte aligned.
  *
  * rattn_ring_pack / rattn_ring_unpack: both rings of N sequences, every slot, from and to the type p->dtype (p->Hq, the scale,

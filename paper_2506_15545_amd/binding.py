@@ -482,7 +482,8 @@ def rattn_ring_pack(k_ring, v_ring, out=None):
 
 
 def rattn_ring_unpack(k_codes, k_scale, v_codes, v_scale, dtype=torch.bfloat16, out=None):
-    """(k_ring, v_ring) in `dtype` of packed rings; both types hold what is packed exactly.  `out`: the two, to be reused."""
+    """(k_ring, v_ring) in `dtype` of packed rings; both types hold what is packed exactly (bf16: but for values below 2^-130, which
+    are rounded to multiples of 2^-133).  `out`: the two, to be reused."""
     if k_codes.dim() != 4 or dtype not in _DTYPES:
         raise ValueError("codes must be [N,Hkv,W,D] and dtype float32 or bfloat16")
     shape = k_codes.shape

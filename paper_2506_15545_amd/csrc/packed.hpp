@@ -3,9 +3,9 @@
 // power of two, from 2^-126 on, with which the largest finite feature of the block is at most 448: the block's largest feature
 // keeps its three bits and nothing overflows.  A factor that is a power of two rounds nothing itself: a value is the nearest E4M3
 // number (ties to even) times it, off by at most 2^-4 of itself or 2^-10 of 2^(b - 127), and both bf16 and fp32 hold it exactly
-// (in fp32 down to 2^-126 times 2^-9, in bf16 its numbers below 2^-133 are zero).  So the matrix cores get it as bf16 without
-// another rounding, and packing what was unpacked gives the same values again: after rounding the largest feature is at most
-// 448 and at least 224, and where it is 224 exactly the next smaller factor holds the block's values too.
+// (fp32 all of them, from 2^-135 on; bf16 rounds those below 2^-130 to multiples of 2^-133, its least step).  So the matrix cores
+// get it as bf16 without another rounding, and packing what was unpacked gives the unpacked values again: after rounding the
+// largest feature is at most 448 and at least 224, and where it is 224 exactly the next smaller factor holds the block's values too.
 // Infinities and NaN become NaN (E4M3 has no infinity, and a finite number would hide them); they do not count for the scale.
 #pragma once
 #include "common.hpp"
