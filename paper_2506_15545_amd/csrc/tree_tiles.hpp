@@ -2,7 +2,7 @@
 // share them, each for 32 rows of its own.
 //
 // Few rows are bound by what a CU takes in; with many every wave would fetch the same ring again (192 pairs, W = 2048, 230 rows each:
-// 2 GB through L1 at 64 bytes a cycle and CU), so here a tile of 64 keys is fetched once for up to 256 rows.  The formulation is the
+// 2 GB through L1 at 64 bytes a cycle and CU), so here a tile of 64 keys is fetched once for a work-group's 128 rows.  The formulation is the
 // layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
 // second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
 // phi(k) of the keys that leave, then the state, both as two bf16 terms.
@@ -24,7 +24,8 @@ constexpr int TILE_WAVES = TREE_TILE_WAVES, TILE_THREADS = 64 * TILE_WAVES;
 constexpr int TILE_GAINS = 8;
 // More work-groups than run at once (two on each of 256 CUs) take the sequences with the longest rings first: one that starts when
 // others end is a short one.  (24 sequences of 100 to 4000 tokens, 8 KV heads, 305 rows, W = 2048, when a work-group took less:
-// 96 us in order, 91 so; then the longest work-groups are what the rest waits for.)
+// 96 us in order, 91 so; then the longest work-groups are what the rest waits for.)  A wave orders as many sequences as it has lanes:
+// more than 64 come in the caller's order (72 of these 331 us, 297 where the caller has them in order of length).
 constexpr unsigned TILE_AT_ONCE = 512;
 template <int D> constexpr size_t tree_tile_lds() { return 4 * (size_t)TileGeom<D>::KT + 2 * TILE_GAINS * D * 4; }
 
