@@ -162,6 +162,38 @@ def cpu_baseline(cfg, units_per_core=6):
             "cpu_model": cpu_model(), "nproc": os.cpu_count()}
 
 
+def calibration_copy(torch):
+    """The out-of-place elementwise pass of --calibrate-copy."""
+    src = torch.zeros(256 * 2 ** 20 // 4, dtype=torch.float32, device="cuda")
+    dst = torch.empty_like(src)
+    torch.add(src, 1.0, out=dst)
+    torch.cuda.synchronize()
+    return {"kernel": "elementwise add, out-of-place", "bytes_read": src.numel() * 4, "bytes_written": dst.numel() * 4}
+
+
+def run_operators(names, steps, warmup, calibrate):
+    """Passes of cases of perf/operators.py through the library; prints microseconds a pass of each as one JSON line."""
+    import torch
+    from perf import operators
+    operators.own = True
+    cases, out = {c["name"]: c for c in operators.listed()}, {}
+    if calibrate:
+        calibration_copy(torch)
+    for name in names:
+        states = [operators.prepare(cases[name], seed) for seed in range(3)]
+        for i in range(warmup):
+            operators.run(states[i % 3])
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        e0.record()
+        for i in range(steps):
+            operators.run(states[i % 3])
+        e1.record()
+        torch.cuda.synchronize()
+        out[name] = e0.elapsed_time(e1) / steps * 1e3
+    print(json.dumps({"us_per_pass": out, "steps": steps, "warmup": warmup}))
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -179,10 +211,16 @@ def main():
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="also run one plain out-of-place elementwise pass over 256 MiB (reads and writes 256 MiB): "
                          "under a counter run its FETCH_SIZE / WRITE_SIZE readings give the counters' scale")
+    ap.add_argument("--operators", metavar="NAMES",
+                    help="instead of the benchmark: --steps passes of each of these cases of perf/operators.py (comma-separated), "
+                         "whose kernels a profiler then sees alone")
     args = ap.parse_args()
     if args.gpus != 1 or int(os.environ.get("WORLD_SIZE", "1")) != 1:
         print("bench.py: this build runs on ONE GPU only (no collectives, no sharding); use --gpus 1", file=sys.stderr)
         sys.exit(2)
+
+    if args.operators:
+        return run_operators(args.operators.split(","), args.steps, args.warmup, args.calibrate_copy)
 
     from paper_2506_15545_amd import synth
     # the CPU baseline forks a worker pool: it runs first, before this process has touched the GPU
@@ -548,12 +586,7 @@ def main():
         out["machine"] = machine
 
     if args.calibrate_copy:
-        src = torch.zeros(256 * 2 ** 20 // 4, dtype=torch.float32, device="cuda")
-        dst = torch.empty_like(src)
-        torch.add(src, 1.0, out=dst)
-        torch.cuda.synchronize()
-        out["calibration"] = {"kernel": "elementwise add, out-of-place", "bytes_read": src.numel() * 4,
-                              "bytes_written": dst.numel() * 4}
+        out["calibration"] = calibration_copy(torch)
 
     if cpu_base is not None:
         out["cpu_baseline"] = cpu_base
