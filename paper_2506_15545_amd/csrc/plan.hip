@@ -157,12 +157,12 @@ TreePlan tree_plan(const TreeDims& td, int dtype, bool packed) {
   const int sets = (int)((td.W + (keys - 1ll)) / keys) + (td.M + keys - 1) / keys;
   const long long pairs = (long long)td.N * td.Hkv;
   // Keys through LDS where waves that fetch them themselves would be more than the chip holds at once (work-groups of 64 rows, one per
-  // CU).  us, direct | tiles, bf16, full rings, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.7 | 38.5, 57.0 | 78.9; of 256
-  // 47.9 | 42.2, 107 | 84; 128 of 128 rows 26.1 | 38.8, 60.4 | 81.2; 136 of 128 44.7 | 39.3, 106 | 80; 192 of 96 45.0 | 39.3, 108 |
-  // 81; 64 of 256 28.5 | 40.9, 57.3 | 82.1; of 512 50.7 | 45.0, 108 | 87.  D = 64: 64 of 256 17.0 | 26.6, 35.6 | 57.2; of 512 31.1 |
-  // 28.8, 69.3 | 61.3 (packed: 17.4 | 29.7, 39.7 | 70.4; of 512 31.4 | 31.9, 73.9 | 72.0).  Packed rings of D = 128, which they unpack
-  // on the way (at the cost of registers), from twice as many on: 192 of 128 45.5 | 48.2, 104 | 111; 256 of 128 48.6 | 49.8, 108 | 115;
-  // 320 of 128 66.1 | 63.7, 155 | 135; 96 of 256 47.4 | 48.0, 101 | 107; 128 of 512 93.5 | 67.8, 212 | 144
+  // CU).  us, direct | tiles, bf16, full rings, D = 128, W = 512 and 2048: 96 pairs of 128 rows 25.5 | 37.5, 56.9 | 75.8; of 256
+  // 48.3 | 41.7, 108 | 80; 128 of 128 rows 26.0 | 37.8, 58.9 | 76.7; 136 of 128 44.4 | 38.1, 106 | 77; 192 of 96 45.3 | 38.5, 107 |
+  // 77; 64 of 256 28.6 | 40.0, 55.1 | 78.8; of 512 51.9 | 44.5, 106 | 83.  D = 64: 64 of 256 17.6 | 26.8, 35.1 | 54.5; of 512 31.4 |
+  // 28.9, 67.6 | 57.7 (packed: 17.7 | 29.6, 39.2 | 69.4; of 512 31.3 | 31.7, 72.8 | 71.0).  Packed rings of D = 128, which they unpack
+  // on the way (at the cost of registers), from twice as many on: 192 of 128 44.9 | 47.3, 105 | 110; 256 of 128 48.7 | 49.6, 106 | 112;
+  // 320 of 128 65.1 | 62.7, 152 | 128; 96 of 256 46.8 | 47.1, 102 | 107; 128 of 512 91.9 | 65.7, 209 | 138
   if (dtype == 1 && rows > 64 && pairs * ((rows + 63) / 64) > (packed && td.D == 128 ? 512 : 256)) {
     p.tiles = 1;
     p.CT = 2;

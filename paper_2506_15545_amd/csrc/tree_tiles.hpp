@@ -6,10 +6,10 @@
 // layer forward's: S^T = K Q^T and O^T += V^T P^T with 32 x 32 tiles, a lane owns one row, and the accumulator registers of P^T are the
 // second product's operand.  Nothing meets across waves: a wave has its rows' whole sums.  After the keys the same buffers hold
 // phi(k) of the keys that leave, then the state, both as two bf16 terms.
-// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 99 us, 365 TFLOP/s; fetching their
+// 24 sequences of 61 nodes, 40 query and 8 KV heads, D = 128, W = 2048 (half of the rings not full): 95 us, 380 TFLOP/s; fetching their
 // own keys the waves take 164.  Bound by the way of a wave through its tiles (products, masks and exponentials, products): the
 // work-groups with full rings, less than half of all, are about one for each CU, and the rest waits for them.  Over the whole launch
-// the matrix units are busy for 27 % of it, the vector units for 38 %, LDS for 12 %.
+// the matrix units are busy for 29 % of it, the vector units for 38 %, LDS for 12 %.
 #pragma once
 #include "tree_group.hpp"
 
@@ -79,6 +79,10 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
   x += dpp_get<0x4E>(x);
   x += dpp_get<0x141>(x);
   return LANES == 16 ? x + dpp_get<0x140>(x) : x;
+}
+__device__ __forceinline__ unsigned pack2(float x, float y) {
+  typedef float pair_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(pair_t{x, y}, bf16x2_t));
 }
 __device__ __forceinline__ void split2(float (&x)[8], bf16x8_t& hi, bf16x8_t& lo) {   // (see TreeMath::two_terms)
   float t[8];
@@ -330,53 +334,45 @@ __global__ __launch_bounds__(TILE_THREADS, 2) void tree_tile_kernel(TreeArgs<bf1
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) acc[ct] *= alpha;
       }
-      // The second products in explicit order: operands are read four products ahead, the second half's exponentials stand between
-      // the first half's products.  Of the two waves of a SIMD the one that is here goes first, so that the other's first products
-      // fill what it leaves (108 -> 99 us).
+      // The second products in explicit order: operands are read three ahead, and the next eight keys' probabilities are formed
+      // between the products of the eight before (all of a half's ahead of its products: 99 -> 95 us).  Of the two waves of a SIMD the
+      // one that is here goes first, so that the other's first products fill what it leaves (101 -> 95; the first products preferred
+      // as well 97).
       // Two bf16 terms for the probabilities, as in the direct kernel, so that a sequence's result does not get worse in a larger
-      // batch: with one the output is off by 2.1e-3 of its norm, with two by the 1.66e-3 of its own rounding (81 | 99 us).
+      // batch: with one the output is off by 2.1e-3 of its norm, with two by the 1.66e-3 of its own rounding (81 | 95 us).
       __builtin_amdgcn_s_setprio(1);
-      constexpr int NP = 2 * NCT, AHEAD = 4;   // products of a half, operands that are read ahead
-      bf16x8_t v[AHEAD], ph[2], pl[2];
-      float pr[16];
-      auto read = [&](int x) {
-        const int i = x % NP;
-        v[x % AHEAD] = tile_trp<D>(V, lo, 32 * (x / NP) + 16 * (i / NCT), i % NCT);
-      };
-      auto prob = [&](int h, int i) { pr[i] = fast_exp2(__builtin_fmaf(s[h][i], sc, -m)); lsum[i & 3] += pr[i]; };
-      auto terms = [&]() {
+      constexpr int AHEAD = 3;   // operands that are read ahead
+      bf16x8_t v[AHEAD];
+      u32x4_t ph[2], pl[2];
+      auto read = [&](int x) { v[x % AHEAD] = tile_trp<D>(V, lo, 16 * (x / NCT), x % NCT); };
+      auto pair_of = [&](int g, int j) {   // keys 2j and 2j + 1 of the g-th eight of this lane's row
+        float p[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = pr[8 * k + i];
-          split2(x, ph[k], pl[k]);
+        for (int i = 0; i < 2; ++i) {
+          p[i] = fast_exp2(__builtin_fmaf(s[g / 2][8 * (g % 2) + 2 * j + i], sc, -m));
+          lsum[2 * (j & 1) + i] += p[i];
         }
-      };
-      auto product = [&](int x) {
-        f32x16_t& o = acc[x % NCT];
-        o = mfma32(v[x % AHEAD], pl[x % NP / NCT], o);
-        o = mfma32(v[x % AHEAD], ph[x % NP / NCT], o);
-        if (x + AHEAD < 2 * NP) read(x + AHEAD);
+        const unsigned hi = (unsigned)opaque((int)pack2(p[0], p[1]));   // (else the compiler rounds each alone once more)
+        ph[g % 2][j] = hi;
+        pl[g % 2][j] = pack2(p[0] - __uint_as_float(hi << 16), p[1] - __uint_as_float(hi & 0xffff0000u));
       };
 #pragma unroll
       for (int x = 0; x < AHEAD; ++x) read(x);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) prob(0, i);
-      terms();
+      for (int j = 0; j < 4; ++j) pair_of(0, j);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < NP; ++x) {
-        product(x);
+      for (int x = 0; x < 4 * NCT; ++x) {
+        const int g = x / NCT, ct = x % NCT;
+        acc[ct] = mfma32(v[x % AHEAD], __builtin_bit_cast(bf16x8_t, pl[g % 2]), acc[ct]);
+        acc[ct] = mfma32(v[x % AHEAD], __builtin_bit_cast(bf16x8_t, ph[g % 2]), acc[ct]);
+        if (x + AHEAD < 4 * NCT) read(x + AHEAD);
+        if (g < 3) {
 #pragma unroll
-        for (int j = 16 / NP * x; j < 16 / NP * (x + 1); ++j) prob(1, j);
+          for (int j = 4 / NCT * ct; j < 4 / NCT * (ct + 1); ++j) pair_of(g + 1, j);
+        }
         __builtin_amdgcn_sched_barrier(0);
-      }
-      terms();
-#pragma unroll
-      for (int x = NP; x < 2 * NP; ++x) {
-        product(x);
       }
       __builtin_amdgcn_s_setprio(0);
     }
